@@ -210,7 +210,7 @@ def run(s):
             return s["p"], s["m"], s["v"]
         if "m32" not in s:
             s["m32"], s["v32"] = torch.zeros_like(s["p"]), torch.zeros_like(s["p"])
-            s["to"] = [(s["m32"][a:a + k], s["v32"][a:a + k]) for a, k in zip(s["start"], s["count"])]
+            s["to"] = s["tensors"].moment_targets([(s["m32"][a:a + k], s["v32"][a:a + k]) for a, k in zip(s["start"], s["count"])])
         s["tensors"].moments(s["to"])
         return s["p"], s["m32"], s["v32"]
     if kind in ("lora", "lora_grad"):

@@ -481,6 +481,153 @@ int prom_block_noalloc(const int8_t *x, int n, int h, int w, int cin, int chid, 
 /* Bytes of the fixed array behind prom_block_noalloc. */
 size_t prom_block_noalloc_max_workspace(void);
 
+/* ---- real-valued tensors -----------------------------------------------------------------
+ * Element types of the entry points below. */
+enum { PROM_F32 = 0, PROM_BF16 = 1, PROM_F16 = 2 };
+
+/* ---- ternary pointwise layer with the low-rank adapters of many requests --------------------
+ * One set of ternary weights serves every batch element, and each element brings the adapter it was fine-tuned with:
+ * with i the batch element of row m (the pixels or tokens of one element follow each other), l = index[i],
+ *   hid[m][r] = x_step[i] * sum_k x[m][k] * a[l][r][k]
+ *   y[m][co]  = (acc[m][co] * w_scale[co]) * x_step[i] + bias[co] + scale[l] * sum_r hid[m][r] * b[l][r][co]
+ * acc the int32 accumulator of prom_pw_conv, everything real in float32 (up to the bias three operations, each rounded once,
+ * as in prom_pw_conv_dynq), one rounding to y's type at the end.
+ * An index outside [0, adapters) means no adapter: the sum over r is left out and hid is zero.  Nothing an adapter
+ * holds (infinities, NaN) reaches rows that do not take it.
+ *   a      dev [adapters][rank][cin] of `type` (PROM_BF16 or PROM_F16)
+ *   b      dev [adapters][rank][cout] of `type`: row r is the r-th direction in the output channels
+ *   scale  dev float32 [adapters];  index dev int32 [n] */
+typedef struct {
+    const void *a;
+    const void *b;
+    const float *scale;
+    const int32_t *index;
+    int32_t adapters, rank, type;
+} prom_lora_t;
+
+/*   x         dev int8 [n][h][w][cin], real value x * x_step[i];  x_step dev float32 [n]
+ *   w_packed  dev, prom_pack_ternary output for [cout][cin];  w_scale dev float32 [cout];  bias dev float32 [cout] or NULL
+ *   y         dev [n][h][w][cout] of y_type: PROM_F32 or the adapters' type
+ *   hid       dev float32 [n*h*w][rank] or NULL: what prom_pw_conv_lora_backward takes
+ *   workspace dev, 256-byte aligned, at least prom_pw_conv_lora_workspace_size(...) bytes (0 for sizes that are refused); contents
+ *             undefined afterwards.  Two calls that can overlap in time need one each.
+ * Any channels, rows, rank and alignment to elements (w_packed: 4 bytes).  PROM_EINVAL for null or misaligned pointers,
+ * non-positive sizes, other types; PROM_EUNSUPPORTED above 65536 channels, rank 128, 65535 adapters or 2^30 - 1 rows; PROM_EALIAS if an
+ * output overlaps an input or another output; PROM_EWORKSPACE. */
+int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, const void *w_packed, int cout, const float *x_step,
+                      const float *w_scale, const float *bias, const prom_lora_t *lora, void *y, int y_type, float *hid,
+                      void *workspace, size_t workspace_bytes, void *stream);
+size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank);
+
+/* Its gradients, with the shared weights frozen and the activations' rounding passed straight through: with
+ * g[m][r] = scale[l] * sum_co dy[m][co] * b[l][r][co],
+ *   dx[m][k]     = sum_co dy[m][co] * w_scale[co] * W[co][k] + sum_r g[m][r] * a[l][r][k]
+ *   da[l][r][k]  = sum over the rows m of adapter l of g[m][r] * x_step[i] * x[m][k]
+ *   db[l][r][co] = scale[l] * sum over the rows m of adapter l of hid[m][r] * dy[m][co]
+ * dx is the gradient of the real activations x * x_step.  Sums in float32 and in a fixed order; dy * w_scale is rounded to 8 bits for a
+ * bf16 dy, 16 for f16, 24 for float32 (no more than the types hold), all else is exact to float32.
+ *   dy, dx     dev [n][h][w][cout] and [n][h][w][cin] of dy_type: PROM_F32 or the adapters' type
+ *   wt_packed  dev, prom_pack_ternary output of the TRANSPOSED weights [cin][cout] (once per layer; not looked at without dx)
+ *   hid        dev float32 [n*h*w][rank], from the forward call (not looked at without db); x is not looked at without da
+ *   da, db     dev float32 [adapters][rank][cin] and [adapters][rank][cout], zeros for an adapter without rows
+ * dx, da and db may each be NULL, not all three.  The rest as above. */
+int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int8_t *x, int n, int h, int w, int cin,
+                               const void *wt_packed, int cout, const float *x_step, const float *w_scale,
+                               const prom_lora_t *lora, const float *hid, void *dx, float *da, float *db,
+                               void *workspace, size_t workspace_bytes, void *stream);
+size_t prom_pw_conv_lora_backward_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank, int dy_type);
+
+/* ---- layer norm ---------------------------------------------------------------------------
+ * Over the rows of x [rows][cols], sums and moments in float32:
+ *   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps)
+ *   y = ((x - mean) * rstd) * weight + bias       four float32 operations, rounded once each, then once to y's type
+ *   x, y        dev [rows][cols] of `type`, aligned to their elements (rows of any width may follow each other)
+ *   weight      dev float32 [cols] or NULL (ones);  bias dev float32 [cols] or NULL (zeros)
+ *   mean, rstd  dev float32 [rows] or NULL: what prom_layernorm_backward takes
+ * No output may overlap an input or another output (PROM_EALIAS).  PROM_EINVAL for null or misaligned pointers,
+ * an unknown type, non-positive sizes, eps < 0; PROM_EUNSUPPORTED above 32768 columns or 2^31 - 1 rows. */
+int prom_layernorm(const void *x, int type, long long rows, int cols, const float *weight, const float *bias, float eps,
+                   void *y, float *mean, float *rstd, void *stream);
+
+/* The same with the rows quantised on the way out, one scale per row (the activation quantiser of paper Section 3.1,
+ * Eq. 6-7, factor 127 and eps clamp as in its pseudocode), for prom_pw_conv_lora and prom_pw_conv_dynq: with y in float32 as above
+ * (mean and rstd summed in float64 and rounded once, so that no code depends on the order of a sum)
+ *   top = max(max_c |y|, quant_eps),  q = clamp(round_half_even(y * (127 / top)), -128, 127),  step = top / 127
+ *   q  dev int8 [rows][cols];  step dev float32 [rows]: the real value is q * step.
+ * A row with a NaN gets the step NaN, one with an infinity an infinite or NaN step; their codes mean nothing. */
+int prom_layernorm_quant(const void *x, int type, long long rows, int cols, const float *weight, const float *bias, float eps,
+                         float quant_eps, int8_t *q, float *step, float *mean, float *rstd, void *stream);
+
+/* Gradients of prom_layernorm (and, straight through the rounding, of prom_layernorm_quant): with h = (x - mean) * rstd and
+ * g = dy * weight,
+ *   dx = rstd * (g - sum_c g / cols - h * sum_c (g * h) / cols),  dweight = sum_rows dy * h,  dbias = sum_rows dy
+ *   dy, x, dx        dev [rows][cols] of `type`;  mean, rstd dev float32 [rows]
+ *   dweight, dbias   dev float32 [cols]; dx, dweight and dbias may each be NULL, not all three
+ *   workspace        dev, 256-byte aligned, at least prom_layernorm_backward_workspace_size(...) bytes; may be NULL
+ *                    when neither dweight nor dbias is asked for.  Contents undefined afterwards.
+ * Sums over rows are added in a fixed order: the same inputs give the same bits.  Errors as above; PROM_EWORKSPACE
+ * for a missing, short or misaligned workspace. */
+int prom_layernorm_backward(const void *dy, const void *x, int type, long long rows, int cols, const float *weight,
+                            const float *mean, const float *rstd, void *dx, float *dweight, float *dbias,
+                            void *workspace, size_t workspace_bytes, void *stream);
+size_t prom_layernorm_backward_workspace_size(int type, long long rows, int cols);
+
+/* ---- AdamW over many tensors ----------------------------------------------------------------
+ * One step, one launch, any number of tensors (the adapters of prom_pw_conv_lora, the weights of prom_layernorm, the float
+ * weights behind prom_quantize_pw_absmean):
+ *   g = grad * grad_scale;  m = m*beta1 + g*(1-beta1);  v = v*beta2 + (g*(1-beta2))*g;  root = sqrt(v)
+ *   p = p*(1 - lr*wd) - (m * (lr/(1-beta1^step))) / (root * (1/sqrt(1-beta2^step)) + eps)
+ * every operation rounded once in float32, the bracketed constants computed in float64 and rounded once; then one
+ * rounding to the parameter's type.
+ * Moments in 8 bits (state_bits 8): blocks of 256 consecutive elements of a tensor share two scales,
+ *   m = c*|c| * avg_scale,   c = sign(m) * min(round(sqrt(|m| * (16129 / top))), 127),    avg_scale = top * (1/16129)
+ *   root = r*r * sq_scale,   r = min(round(sqrt(root * (65025 / top))), 255), at least 1 where root > 0,  v = root*root
+ * with top the largest |m| and root of the block, all in float32, each operation rounded once; a block whose top is below
+ * 2^-100 is held as zeros.  All-zero codes and scales are the initial state.  The step itself uses the moments before they are rounded to codes.  A NaN or an
+ * infinity among a block's moments makes its scale NaN. */
+typedef struct {
+    void *param;              /* dev [n] of param_type, updated                                        */
+    const void *grad;         /* dev [n] of grad_type                                                  */
+    void *exp_avg;            /* dev m: float32 [n], or int8 [n] when state_bits is 8                  */
+    void *exp_avg_sq;         /* dev v: float32 [n], or uint8 [n] (codes of its root)                  */
+    float *avg_scale;         /* dev [ceil(n / 256)] when state_bits is 8                              */
+    float *sq_scale;          /* dev [ceil(n / 256)] when state_bits is 8                              */
+    void *copy;               /* dev [n] of copy_type or NULL: also receives the new parameter          */
+    long long n;
+    int32_t param_type, grad_type, copy_type, state_bits;
+} prom_adamw_tensor_t;
+
+typedef struct {
+    int32_t tensors, workgroups;
+} prom_adamw_plan_t;
+
+/* Hyperparameters; read on the host at call time, except what the three device pointers stand for, which the
+ * kernel reads: with step_dev (dev int32, the step's number from 1 on) and lr_dev a captured step follows its schedule. */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int32_t step;             /* from 1 on; not looked at with step_dev                                */
+    const int32_t *step_dev;  /* dev or NULL                                                           */
+    const float *lr_dev;      /* dev or NULL: used instead of lr                                       */
+    const float *grad_scale;  /* dev or NULL: 1                                                        */
+} prom_adamw_hyper_t;
+
+/* The table of a set of tensors: written on the host once (prom_adamw_table_size bytes), copied to the device by the
+ * caller (8-byte aligned) and passed to every step with the plan.  It holds the tensors' addresses: build it anew when one moves.
+ * Tensors may lie anywhere, aligned to their elements; an output that overlaps its tensor's gradient or another of its outputs is
+ * PROM_EALIAS (tensors are not compared with each other: they must not overlap).  PROM_EINVAL for null or misaligned pointers,
+ * n <= 0, an unknown type or state_bits; the offending tensor's index goes to *bad_tensor if not NULL.  0 bytes where prom_adamw_table would fail. */
+size_t prom_adamw_table_size(const prom_adamw_tensor_t *tensors, int count);
+int prom_adamw_table(const prom_adamw_tensor_t *tensors, int count, void *table_host, size_t table_bytes,
+                     prom_adamw_plan_t *plan, int *bad_tensor);
+
+/* One step.  table: the device copy; it must be the one that plan was filled with (not checked). */
+int prom_adamw_step(const void *table, const prom_adamw_plan_t *plan, const prom_adamw_hyper_t *hyper, void *stream);
+
+/* The moments of every tensor in float32, for checkpoints: exp_avg, exp_avg_sq are device arrays of plan->tensors device
+ * pointers, each to float32 [n]. */
+int prom_adamw_moments(const void *table, const prom_adamw_plan_t *plan, float *const *exp_avg,
+                       float *const *exp_avg_sq, void *stream);
+
 /* ---- measurement utility ------------------------------------------------------------------
  * Plain streaming copy of nbytes (multiple of 16, both pointers 16-byte aligned) from src to
  * dst, dev to dev, as a kernel of this library: the HBM-bandwidth yardstick the pointwise

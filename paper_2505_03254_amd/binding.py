@@ -58,6 +58,27 @@ class _GconvLayerC(ctypes.Structure):
                 ("rq", _RequantC), ("y", ctypes.c_void_p)]
 
 
+class _LoraC(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("index", ctypes.c_void_p),
+                ("adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _AdamWTensorC(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("avg_scale", ctypes.c_void_p), ("sq_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_longlong),
+                ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("copy_type", ctypes.c_int32), ("state_bits", ctypes.c_int32)]
+
+
+class _AdamWPlanC(ctypes.Structure):
+    _fields_ = [("tensors", ctypes.c_int32), ("workgroups", ctypes.c_int32)]
+
+
+class _AdamWHyperC(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int32), ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_void_p)]
+
+
 class _PlanC(ctypes.Structure):
     _fields_ = [("tiles_per_wave", ctypes.c_int32), ("pixel_tiles", ctypes.c_int32),
                 ("workgroups", ctypes.c_int32), ("row_waves", ctypes.c_int32), ("k_outer", ctypes.c_int32)]
@@ -170,6 +191,31 @@ def load_library():
     lib.prom_mfma_i8_loop.argtypes = [ci, vp, vp]
     lib.prom_requant_check.restype = ci
     lib.prom_requant_check.argtypes = [ctypes.POINTER(_RequantC), ci, ci, ctypes.POINTER(ci)]
+    cll, cf = ctypes.c_longlong, ctypes.c_float
+    lib.prom_pw_conv_lora.restype = ci
+    lib.prom_pw_conv_lora.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, vp, ctypes.POINTER(_LoraC), vp, ci, vp, vp, sz, vp]
+    lib.prom_pw_conv_lora_workspace_size.restype = sz
+    lib.prom_pw_conv_lora_workspace_size.argtypes = [ci] * 7
+    lib.prom_pw_conv_lora_backward.restype = ci
+    lib.prom_pw_conv_lora_backward.argtypes = [vp, ci, vp, ci, ci, ci, ci, vp, ci, vp, vp, ctypes.POINTER(_LoraC), vp, vp, vp, vp, vp, sz, vp]
+    lib.prom_pw_conv_lora_backward_workspace_size.restype = sz
+    lib.prom_pw_conv_lora_backward_workspace_size.argtypes = [ci] * 8
+    lib.prom_layernorm.restype = ci
+    lib.prom_layernorm.argtypes = [vp, ci, cll, ci, vp, vp, cf, vp, vp, vp, vp]
+    lib.prom_layernorm_quant.restype = ci
+    lib.prom_layernorm_quant.argtypes = [vp, ci, cll, ci, vp, vp, cf, cf, vp, vp, vp, vp, vp]
+    lib.prom_layernorm_backward.restype = ci
+    lib.prom_layernorm_backward.argtypes = [vp, vp, ci, cll, ci, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.prom_layernorm_backward_workspace_size.restype = sz
+    lib.prom_layernorm_backward_workspace_size.argtypes = [ci, cll, ci]
+    lib.prom_adamw_table_size.restype = sz
+    lib.prom_adamw_table_size.argtypes = [ctypes.POINTER(_AdamWTensorC), ci]
+    lib.prom_adamw_table.restype = ci
+    lib.prom_adamw_table.argtypes = [ctypes.POINTER(_AdamWTensorC), ci, vp, sz, ctypes.POINTER(_AdamWPlanC), ctypes.POINTER(ci)]
+    lib.prom_adamw_step.restype = ci
+    lib.prom_adamw_step.argtypes = [vp, ctypes.POINTER(_AdamWPlanC), ctypes.POINTER(_AdamWHyperC), vp]
+    lib.prom_adamw_moments.restype = ci
+    lib.prom_adamw_moments.argtypes = [vp, ctypes.POINTER(_AdamWPlanC), vp, vp, vp]
     lib.prom_strerror.restype = ctypes.c_char_p
     lib.prom_strerror.argtypes = [ci]
     lib.prom_last_hip_error.restype = ctypes.c_char_p
@@ -561,6 +607,311 @@ def prom_pw_conv_dynq(x, w_packed, cout: int, x_step, w_scale, bias=None, relu: 
         bias.data_ptr() if bias is not None else None, int(bool(relu)), float(eps), q.data_ptr(),
         amax.data_ptr(), scale.data_ptr(), _stream_ptr(stream)), "prom_pw_conv_dynq")
     return q, amax, scale
+
+
+# ---- real-valued tensors ------------------------------------------------------------------------
+PROM_F32, PROM_BF16, PROM_F16 = 0, 1, 2
+_types = None
+
+
+def _type_of(dtype) -> int:
+    global _types
+    if _types is None:
+        torch = _torch or _import_torch()
+        _types = {torch.float32: PROM_F32, torch.bfloat16: PROM_BF16, torch.float16: PROM_F16}
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise TypeError(f"{dtype} is not float32, bfloat16 or float16") from None
+
+
+def _dev(t, name, dtype=None, shape=None, device=None):
+    """t as a contiguous device tensor, checked; its address."""
+    if not (t.is_cuda and t.is_contiguous()) or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be a contiguous {dtype or 'device'} tensor on a GPU")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {list(shape)}, not {list(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the input on {device}")
+    return t.data_ptr()
+
+
+def _opt(t, name, dtype, shape, device):
+    return None if t is None else _dev(t, name, dtype, shape, device)
+
+
+class _OnDevice:
+    """The calls launch on the device that is current: make it that of the tensors (nothing to do in the usual case)."""
+
+    def __init__(self, device):
+        torch = _torch or _import_torch()
+        torch.cuda._lazy_init()
+        self.to = device.index
+        self.back = torch._C._cuda_getDevice()
+
+    def __enter__(self):
+        if self.to != self.back:
+            _torch.cuda.set_device(self.to)
+
+    def __exit__(self, *exc):
+        if self.to != self.back:
+            _torch.cuda.set_device(self.back)
+
+
+def _norm_rows(x, name="x"):
+    if x.dim() < 1 or x.numel() == 0:
+        raise ValueError(f"{name} must have rows and columns")
+    cols = x.shape[-1]
+    return x.numel() // cols, cols
+
+
+def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, rstd=None, stream=None):
+    """Layer norm over the last dimension of x (float32, bfloat16 or float16; weight and bias float32 or None).
+    Returns (y, mean, rstd); mean and rstd float32, one per row."""
+    torch = _torch or _import_torch()
+    px, d = _dev(x, "x"), x.device
+    rows, cols = _norm_rows(x)
+    f32 = torch.float32
+    y = torch.empty_like(x) if y is None else y
+    mean = torch.empty(rows, dtype=f32, device=d) if mean is None else mean
+    rstd = torch.empty(rows, dtype=f32, device=d) if rstd is None else rstd
+    with _OnDevice(d):
+        _check(load_library().prom_layernorm(
+            px, _type_of(x.dtype), rows, cols, _opt(weight, "weight", f32, (cols,), d), _opt(bias, "bias", f32, (cols,), d), float(eps),
+            _dev(y, "y", x.dtype, x.shape, d), _dev(mean, "mean", f32, (rows,), d), _dev(rstd, "rstd", f32, (rows,), d), _stream_ptr(stream)),
+            "prom_layernorm")
+    return y, mean, rstd
+
+
+def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps: float = 1e-5, q=None, step=None, mean=None, rstd=None,
+                         stream=None):
+    """The same with every row quantised to int8.  Returns (q int8 of x's shape, step, mean, rstd): the real value is
+    q * step, row by row."""
+    torch = _torch or _import_torch()
+    px, d = _dev(x, "x"), x.device
+    rows, cols = _norm_rows(x)
+    f32 = torch.float32
+    q = torch.empty(x.shape, dtype=torch.int8, device=d) if q is None else q
+    step = torch.empty(rows, dtype=f32, device=d) if step is None else step
+    mean = torch.empty(rows, dtype=f32, device=d) if mean is None else mean
+    rstd = torch.empty(rows, dtype=f32, device=d) if rstd is None else rstd
+    with _OnDevice(d):
+        _check(load_library().prom_layernorm_quant(
+            px, _type_of(x.dtype), rows, cols, _opt(weight, "weight", f32, (cols,), d), _opt(bias, "bias", f32, (cols,), d), float(eps),
+            float(quant_eps), _dev(q, "q", torch.int8, x.shape, d), _dev(step, "step", f32, (rows,), d), _dev(mean, "mean", f32, (rows,), d),
+            _dev(rstd, "rstd", f32, (rows,), d), _stream_ptr(stream)), "prom_layernorm_quant")
+    return q, step, mean, rstd
+
+
+def prom_layernorm_backward_workspace_size(dtype, rows: int, cols: int) -> int:
+    return int(load_library().prom_layernorm_backward_workspace_size(_type_of(dtype), rows, cols))
+
+
+def prom_layernorm_backward(dy, x, weight, mean, rstd, want_dx: bool = True, want_dweight: bool = True, want_dbias: bool = True,
+                            workspace=None, stream=None):
+    """Gradients of prom_layernorm.  Returns (dx, dweight, dbias), None for what is not wanted."""
+    torch = _torch or _import_torch()
+    px, d = _dev(x, "x"), x.device
+    rows, cols = _norm_rows(x)
+    f32 = torch.float32
+    pdy = _dev(dy, "dy", x.dtype, x.shape, d)
+    dx = torch.empty_like(x) if want_dx else None
+    dweight = torch.empty(cols, dtype=f32, device=d) if want_dweight else None
+    dbias = torch.empty(cols, dtype=f32, device=d) if want_dbias else None
+    lib = load_library()
+    t = _type_of(x.dtype)
+    if workspace is None and (want_dweight or want_dbias):
+        workspace = torch.empty(lib.prom_layernorm_backward_workspace_size(t, rows, cols), dtype=torch.uint8, device=d)
+    with _OnDevice(d):
+        _check(lib.prom_layernorm_backward(
+            pdy, px, t, rows, cols, _opt(weight, "weight", f32, (cols,), d), _dev(mean, "mean", f32, (rows,), d), _dev(rstd, "rstd", f32, (rows,), d),
+            None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+            None if workspace is None else _dev(workspace, "workspace", device=d),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_layernorm_backward")
+    return dx, dweight, dbias
+
+
+@dataclass
+class Lora:
+    """The adapters of many requests: a [adapters][rank][cin], b [adapters][rank][cout] (bfloat16 or float16), scale
+    float32 [adapters], index int32 [n]: the adapter of each batch element, anything outside [0, adapters) for none."""
+    a: "torch.Tensor"
+    b: "torch.Tensor"
+    scale: "torch.Tensor"
+    index: "torch.Tensor"
+
+    def _c(self, n, cin, cout, device) -> _LoraC:
+        torch = _torch or _import_torch()
+        a, b = self.a, self.b
+        if a.dim() != 3:
+            raise ValueError("a must be [adapters, rank, cin]")
+        adapters, rank = a.shape[0], a.shape[1]
+        return _LoraC(_dev(a, "a", None, (adapters, rank, cin), device), _dev(b, "b", a.dtype, (adapters, rank, cout), device),
+                      _dev(self.scale, "scale", torch.float32, (adapters,), device), _dev(self.index, "index", torch.int32, (n,), device),
+                      adapters, rank, _type_of(a.dtype))
+
+
+def prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank) -> int:
+    return int(load_library().prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank))
+
+
+def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora, dtype=None, y=None, hid=None, want_hid: bool = False,
+                      workspace=None, stream=None):
+    """x int8 [n,h,w,cin] device, x_step float32 [n], w_scale float32 [cout], bias float32 [cout] or None.  y is of `dtype`: the adapters' type (default)
+    or float32.  Returns y, or (y, hid float32 [n*h*w, rank]) with want_hid or a hid of the caller's."""
+    torch = _torch or _import_torch()
+    _dev_i8(x, "x")
+    d = x.device
+    n, h, w, cin = x.shape
+    lc = lora._c(n, cin, cout, d)
+    f32 = torch.float32
+    if y is None:
+        y = torch.empty((n, h, w, cout), dtype=dtype or lora.a.dtype, device=d)
+    want_hid = want_hid or hid is not None
+    if want_hid and hid is None:
+        hid = torch.empty((n * h * w, lc.rank), dtype=f32, device=d)
+    lib = load_library()
+    if workspace is None:
+        workspace = torch.empty(lib.prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank), dtype=torch.uint8, device=d)
+    if w_packed.numel() * w_packed.element_size() < cout * ((cin + 15) // 16) * 4:
+        raise ValueError("w_packed is smaller than the packed form of [cout, cin]")
+    with _OnDevice(d):
+        _check(lib.prom_pw_conv_lora(
+            x.data_ptr(), n, h, w, cin, _dev(w_packed, "w_packed", device=d), int(cout), _dev(x_step, "x_step", f32, (n,), d),
+            _dev(w_scale, "w_scale", f32, (cout,), d), _opt(bias, "bias", f32, (cout,), d), ctypes.byref(lc), _dev(y, "y", None, (n, h, w, cout), d),
+            _type_of(y.dtype), _opt(hid, "hid", f32, (n * h * w, lc.rank), d), _dev(workspace, "workspace", device=d),
+            workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_pw_conv_lora")
+    return (y, hid) if want_hid else y
+
+
+def prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, adapters, rank, dtype) -> int:
+    return int(load_library().prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, adapters, rank, _type_of(dtype)))
+
+
+def prom_pw_conv_lora_backward(dy, x, x_step, wt_packed, w_scale, lora: Lora, hid, want_dx: bool = True, want_da: bool = True, want_db: bool = True,
+                               workspace=None, stream=None):
+    """Gradients of prom_pw_conv_lora: dy [n,h,w,cout] float32 or of the adapters' type; wt_packed: prom_pack_ternary of the transposed weights
+    [cin, cout].  Returns (dx of dy's type [n,h,w,cin], da, db float32 of the adapters' shapes), None for what is not wanted."""
+    torch = _torch or _import_torch()
+    _dev_i8(x, "x")
+    d = x.device
+    n, h, w, cin = x.shape
+    cout = dy.shape[-1]
+    lc = lora._c(n, cin, cout, d)
+    f32 = torch.float32
+    pdy, t = _dev(dy, "dy", None, (n, h, w, cout), d), _type_of(dy.dtype)
+    dx = torch.empty((n, h, w, cin), dtype=dy.dtype, device=d) if want_dx else None
+    da = torch.empty(lora.a.shape, dtype=f32, device=d) if want_da else None
+    db = torch.empty(lora.b.shape, dtype=f32, device=d) if want_db else None
+    lib = load_library()
+    if workspace is None:
+        workspace = torch.empty(lib.prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank, t), dtype=torch.uint8, device=d)
+    if want_dx and wt_packed.numel() * wt_packed.element_size() < cin * ((cout + 15) // 16) * 4:
+        raise ValueError("wt_packed is smaller than the packed form of [cin, cout]")
+    with _OnDevice(d):
+        _check(lib.prom_pw_conv_lora_backward(
+            pdy, t, x.data_ptr(), n, h, w, cin, _opt(wt_packed, "wt_packed", None, None, d), cout, _dev(x_step, "x_step", f32, (n,), d),
+            _opt(w_scale, "w_scale", f32, (cout,), d), ctypes.byref(lc), _opt(hid, "hid", f32, (n * h * w, lc.rank), d),
+            None if dx is None else dx.data_ptr(), None if da is None else da.data_ptr(), None if db is None else db.data_ptr(),
+            _dev(workspace, "workspace", device=d), workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_pw_conv_lora_backward")
+    return dx, da, db
+
+
+@dataclass
+class AdamWTensor:
+    """One tensor of an AdamW step.  exp_avg, exp_avg_sq: float32 of the parameter's size, or int8 and uint8 with avg_scale,
+    sq_scale float32 [ceil(n / 256)]; copy (optional): also receives the new parameter, in its own type."""
+    param: "torch.Tensor"
+    grad: "torch.Tensor"
+    exp_avg: "torch.Tensor"
+    exp_avg_sq: "torch.Tensor"
+    avg_scale: "Optional[torch.Tensor]" = None
+    sq_scale: "Optional[torch.Tensor]" = None
+    copy: "Optional[torch.Tensor]" = None
+
+    def _c(self, device) -> _AdamWTensorC:
+        torch = _torch or _import_torch()
+        n = self.param.numel()
+        p, g = _dev(self.param, "param", device=device), _dev(self.grad, "grad", device=device)
+        if self.grad.numel() != n or (self.copy is not None and self.copy.numel() != n):
+            raise ValueError("param, grad and copy must have the same size")
+        bits = 8 if self.exp_avg.dtype == torch.int8 else 32
+        m = _dev(self.exp_avg, "exp_avg", torch.int8 if bits == 8 else torch.float32, device=device)
+        v = _dev(self.exp_avg_sq, "exp_avg_sq", torch.uint8 if bits == 8 else torch.float32, device=device)
+        if self.exp_avg.numel() != n or self.exp_avg_sq.numel() != n:
+            raise ValueError("the moments must have the parameter's size")
+        blocks = ((n + 255) // 256,)
+        if bits == 8 and (self.avg_scale is None or self.sq_scale is None):
+            raise ValueError("moments in 8 bits need avg_scale and sq_scale")
+        ms = _dev(self.avg_scale, "avg_scale", torch.float32, blocks, device) if bits == 8 else None
+        vs = _dev(self.sq_scale, "sq_scale", torch.float32, blocks, device) if bits == 8 else None
+        return _AdamWTensorC(p, g, m, v, ms, vs, _opt(self.copy, "copy", None, None, device), n, _type_of(self.param.dtype), _type_of(self.grad.dtype),
+                             _type_of(self.copy.dtype) if self.copy is not None else PROM_F32, bits)
+
+
+class AdamWTensors:
+    """The table of a set of tensors, built and copied to their device once; step() updates all of them with one launch.
+    Keeps references to every tensor it points at."""
+
+    def __init__(self, tensors):
+        torch = _torch or _import_torch()
+        self._keep = list(tensors)
+        if not self._keep:
+            raise ValueError("no tensors")
+        self.device = self._keep[0].param.device
+        self.count = len(self._keep)
+        arr = (_AdamWTensorC * self.count)(*[t._c(self.device) for t in self._keep])
+        lib = load_library()
+        self._plan = _AdamWPlanC()
+        bad = ctypes.c_int(-1)
+        host = np.zeros(max(1, lib.prom_adamw_table_size(arr, self.count)), dtype=np.uint8)
+        rc = lib.prom_adamw_table(arr, self.count, host.ctypes.data, host.size, ctypes.byref(self._plan), ctypes.byref(bad))
+        if rc != PROM_OK:
+            raise PromError(rc, f"prom_adamw_table (tensor {bad.value})")
+        self._table = torch.from_numpy(host).to(self.device)
+
+    def step(self, step, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+             grad_scale=None, stream=None):
+        """step: the step's number, from 1 on, or an int32 device tensor that holds it (a captured step then follows it); lr: a number or a
+        float32 device tensor; grad_scale: None or a float32 device tensor that every gradient is multiplied by."""
+        torch = _torch or _import_torch()
+        d = self.device
+        h = _AdamWHyperC(0.0, float(beta1), float(beta2), float(eps), float(weight_decay), 0, None, None, None)
+        if isinstance(step, torch.Tensor):
+            h.step_dev = _dev(step, "step", torch.int32, None, d)
+        else:
+            h.step = int(step)
+        if isinstance(lr, torch.Tensor):
+            h.lr_dev = _dev(lr, "lr", torch.float32, None, d)
+        else:
+            h.lr = float(lr)
+        if grad_scale is not None:
+            h.grad_scale = _dev(grad_scale, "grad_scale", torch.float32, None, d)
+        with _OnDevice(d):
+            _check(load_library().prom_adamw_step(self._table.data_ptr(), ctypes.byref(self._plan), ctypes.byref(h), _stream_ptr(stream)),
+                   "prom_adamw_step")
+
+    def moment_targets(self, targets):
+        """targets: an (exp_avg, exp_avg_sq) pair of float32 tensors for every tensor.  What moments() takes."""
+        torch = _torch or _import_torch()
+        targets = list(targets)
+        if len(targets) != self.count:
+            raise ValueError(f"{self.count} pairs are needed")
+        for (m, v), t in zip(targets, self._keep):
+            for name, o in (("exp_avg", m), ("exp_avg_sq", v)):
+                _dev(o, name, torch.float32, None, self.device)
+                if o.numel() != t.param.numel():
+                    raise ValueError("a moment's target must have the parameter's size")
+        at = torch.tensor([[m.data_ptr() for m, _ in targets], [v.data_ptr() for _, v in targets]], dtype=torch.int64, device=self.device)
+        return targets, at
+
+    def moments(self, targets, stream=None):
+        """The moments of every tensor in float32, into moment_targets(...)."""
+        keep, at = targets
+        with _OnDevice(self.device):
+            _check(load_library().prom_adamw_moments(self._table.data_ptr(), ctypes.byref(self._plan), at[0].data_ptr(), at[1].data_ptr(),
+                                                     _stream_ptr(stream)), "prom_adamw_moments")
+        return keep
 
 
 def prom_quantize_dw_absmax(w, eps: float = 1e-5, stream=None):

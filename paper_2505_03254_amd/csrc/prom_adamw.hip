@@ -1,0 +1,352 @@
+// One AdamW step over many tensors with one launch, moments in 32 or in 8 bits.
+//
+//   g = grad * grad_scale,  m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2
+//   p' = p (1 - lr wd) - (lr / (1 - beta1^t)) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+//
+// Bound by memory: 28 bytes per element with float32 gradients and moments, 16 (14 with 16-bit gradients) with moments in
+// 8 bits.  A wavefront takes units of 256 consecutive elements of a tensor, 4 per lane: every array is read and
+// written in whole runs, and a unit is the block that shares a scale, so that its maximum never leaves the wavefront.
+// A workgroup's kAdamUnits units are loaded before the first is used.  Which tensor a workgroup works on stands in a
+// table in device memory that the caller builds once: one launch however many tensors there are, two dependent
+// loads per workgroup, which the other workgroups of the compute unit hide.
+//
+// 8 bits: m = c |c| S with a signed code c, |c| <= 127, and S = max |m| / 127^2;  sqrt(v) = c^2 S with c <= 255 and
+// S = max sqrt(v) / 255^2.  Squared codes put half of the steps below a quarter of the maximum: a value of 1/100 of its
+// block's maximum is held to 4 % (m) and 2 % (sqrt(v)), where equal steps hold it to 40 % and 20 %.  A positive v
+// never gets the code 0: the next step would divide by eps alone.  Codes are decided by separately rounded float32
+// operations.
+#include "prom.h"
+#include "prom_float.h"
+#include "prom_launch.h"
+
+#include <cmath>
+#include <cstring>
+#include <type_traits>
+
+namespace prom {
+
+constexpr int kAdamBlock = 256;  // elements of a unit
+constexpr int kAdamUnits = 4;    // units of a wavefront
+constexpr int kAdamChunk = 4 * kAdamUnits * kAdamBlock;  // elements of a workgroup of 4 wavefronts
+
+struct AdamTensor {  // in device memory
+    void *p;
+    const void *g;
+    void *m, *v;
+    float *ms, *vs;
+    void *copy;
+    long long n;
+    int first;  // its first workgroup
+    int8_t ptype, gtype, ctype, bits;
+};
+static_assert(sizeof(AdamTensor) == 72, "the table's layout");
+
+struct AdamHyper {
+    float decay, beta1, omb1, beta2, omb2, eps, step_size, inv_root2;
+    const int *step;  // dev or NULL: decay, step_size and inv_root2 are then computed from lr, wd and the betas
+    const float *lr, *grad_scale;
+    double lr_h, wd, b1, b2;
+    int step_h;
+};
+
+// b^n by squaring; the same operations on the host and on the device
+__host__ __device__ inline double power(double b, int n)
+{
+    double r = 1.0;
+    for (; n > 0; n >>= 1) {
+        if (n & 1) r = r * b;
+        b = b * b;
+    }
+    return r;
+}
+__host__ __device__ inline void corrections(double lr, double wd, double b1, double b2, int t, float *decay, float *step_size, float *inv_root2)
+{
+    *decay = (float)(1.0 - lr * wd);
+    *step_size = (float)(lr / (1.0 - power(b1, t)));
+    *inv_root2 = (float)(1.0 / sqrt(1.0 - power(b2, t)));
+}
+
+// 4 elements from place i of a tensor of n
+__device__ __forceinline__ void load4(const void *p, int type, long long i, long long n, float (&out)[4])
+{
+    const int have = (int)min(n - i, 4LL);
+    auto go = [&](auto t) __attribute__((always_inline)) {
+        Piece<decltype(t), 4> q;
+        q.load_some(static_cast<const decltype(t) *>(p) + i, have);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = (float)q.e[e];
+    };
+    if (type == PROM_F32) go(float{});
+    else if (type == PROM_BF16) go(bf16_t{});
+    else go(f16_t{});
+}
+__device__ __forceinline__ void store4(void *p, int type, long long i, long long n, const float (&v)[4])
+{
+    const int have = (int)min(n - i, 4LL);
+    auto go = [&](auto t) __attribute__((always_inline)) {
+        Piece<decltype(t), 4> q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q.e[e] = (decltype(t))v[e];
+        q.store_some(static_cast<decltype(t) *>(p) + i, have);
+    };
+    if (type == PROM_F32) go(float{});
+    else if (type == PROM_BF16) go(bf16_t{});
+    else go(f16_t{});
+}
+
+// m and sqrt(v) of a lane's 4 codes
+__device__ __forceinline__ void decode_moments(const int8_t *c, const uint8_t *r, float ms, float vs, float (&m)[4], float (&root)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int a = c[e], b = r[e];
+        m[e] = mul_f32((float)(a * (a < 0 ? -a : a)), ms);
+        root[e] = mul_f32((float)(b * b), vs);
+    }
+}
+
+template <int BITS>
+__device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper &h, float decay, float step_size, float inv_root2, float gs,
+                                           long long base, int lane)
+{
+    float p[kAdamUnits][4], g[kAdamUnits][4], m[kAdamUnits][4], v[kAdamUnits][4];
+    Piece<int8_t, 4> mc[kAdamUnits];
+    Piece<uint8_t, 4> vc[kAdamUnits];
+    float ms[kAdamUnits], vs[kAdamUnits];
+#pragma unroll
+    for (int u = 0; u < kAdamUnits; ++u) {
+        const long long i = base + u * kAdamBlock + 4 * lane;
+        if (base + u * kAdamBlock >= t.n) continue;
+        const int have = (int)min(t.n - i, 4LL);
+        load4(t.p, t.ptype, i, t.n, p[u]);
+        load4(t.g, t.gtype, i, t.n, g[u]);
+        if constexpr (BITS == 8) {
+            mc[u].load_some(static_cast<const int8_t *>(t.m) + i, have);
+            vc[u].load_some(static_cast<const uint8_t *>(t.v) + i, have);
+            const long long b = (base + u * kAdamBlock) / kAdamBlock;
+            ms[u] = t.ms[b];
+            vs[u] = t.vs[b];
+        } else {
+            load4(t.m, PROM_F32, i, t.n, m[u]);
+            load4(t.v, PROM_F32, i, t.n, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kAdamUnits; ++u) {
+        const long long i = base + u * kAdamBlock + 4 * lane;
+        if (base + u * kAdamBlock >= t.n) continue;
+        const int have = (int)min(t.n - i, 4LL);
+        if constexpr (BITS == 8) {
+            decode_moments(mc[u].e, vc[u].e, ms[u], vs[u], m[u], v[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = mul_f32(v[u][e], v[u][e]);
+        }
+        float root[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float ge = mul_f32(g[u][e], gs);
+            m[u][e] = add_f32(mul_f32(m[u][e], h.beta1), mul_f32(ge, h.omb1));
+            v[u][e] = add_f32(mul_f32(v[u][e], h.beta2), mul_f32(mul_f32(ge, h.omb2), ge));
+            root[e] = sqrt_f32(v[u][e]);
+            const float denom = add_f32(mul_f32(root[e], inv_root2), h.eps);
+            p[u][e] = sub_f32(mul_f32(p[u][e], decay), __fdiv_rn(mul_f32(m[u][e], step_size), denom));
+        }
+        store4(t.p, t.ptype, i, t.n, p[u]);
+        if (t.copy) store4(t.copy, t.ctype, i, t.n, p[u]);
+        if constexpr (BITS == 32) {
+            store4(t.m, PROM_F32, i, t.n, m[u]);
+            store4(t.v, PROM_F32, i, t.n, v[u]);
+        } else {
+            float mt = 0.0f, vt = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < have) {
+                    mt = bits_max(mt, fabsf(m[u][e]));
+                    vt = bits_max(vt, fabsf(root[e]));
+                }
+            mt = wave_max_bits(mt);
+            vt = wave_max_bits(vt);
+            // below 2^-100 the inverse could overflow: such a block is held as zeros.  An infinity or a NaN makes the
+            // scale NaN, and with it every moment of the block from the next step on, as it would in 32 bits for its element.
+            constexpr float tiny = 0x1p-100f, huge = 0x1.fffffep127f;
+            const float minv = mt < tiny ? 0.0f : __fdiv_rn(16129.0f, mt), vinv = vt < tiny ? 0.0f : __fdiv_rn(65025.0f, vt);
+            const bool mfine = mt <= huge, vfine = vt <= huge;
+            Piece<int8_t, 4> co;
+            Piece<uint8_t, 4> ro;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float c = fminf(rintf(sqrt_f32(mul_f32(fabsf(m[u][e]), minv))), 127.0f);
+                float r = fminf(rintf(sqrt_f32(mul_f32(root[e], vinv))), 255.0f);
+                r = root[e] > 0.0f && vinv > 0.0f ? fmaxf(r, 1.0f) : r;
+                co.e[e] = mfine ? (int8_t)(m[u][e] < 0.0f ? -(int)c : (int)c) : (int8_t)0;
+                ro.e[e] = vfine ? (uint8_t)(int)r : (uint8_t)0;
+            }
+            co.store_some(static_cast<int8_t *>(t.m) + i, have);
+            ro.store_some(static_cast<uint8_t *>(t.v) + i, have);
+            if (lane == 0) {
+                const long long b = (base + u * kAdamBlock) / kAdamBlock;
+                const float nan = __int_as_float(0x7fc00000);
+                t.ms[b] = !mfine ? nan : mt < tiny ? 0.0f : mul_f32(mt, 1.0f / 16129.0f);
+                t.vs[b] = !vfine ? nan : vt < tiny ? 0.0f : mul_f32(vt, 1.0f / 65025.0f);
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamTensor *__restrict__ tensors, const int *__restrict__ owner, const AdamHyper h)
+{
+    const AdamTensor t = tensors[owner[blockIdx.x]];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long base = (long long)((int)blockIdx.x - t.first) * kAdamChunk + wave * kAdamUnits * kAdamBlock;
+    if (base >= t.n) return;
+    float decay = h.decay, step_size = h.step_size, inv_root2 = h.inv_root2;
+    if (h.step || h.lr) corrections(h.lr ? (double)*h.lr : h.lr_h, h.wd, h.b1, h.b2, h.step ? *h.step : h.step_h, &decay, &step_size, &inv_root2);
+    const float gs = h.grad_scale ? *h.grad_scale : 1.0f;
+    if (t.bits == 8) adam_units<8>(t, h, decay, step_size, inv_root2, gs, base, lane);
+    else adam_units<32>(t, h, decay, step_size, inv_root2, gs, base, lane);
+}
+
+// The moments of every tensor in float32: what a checkpoint holds.
+__global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamTensor *__restrict__ tensors, const int *__restrict__ owner,
+                                                            float *const *__restrict__ m_out, float *const *__restrict__ v_out)
+{
+    const int id = owner[blockIdx.x];
+    const AdamTensor t = tensors[id];
+    float *mo = m_out[id], *vo = v_out[id];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long base = (long long)((int)blockIdx.x - t.first) * kAdamChunk + wave * kAdamUnits * kAdamBlock;
+#pragma unroll
+    for (int u = 0; u < kAdamUnits; ++u) {
+        const long long b0 = base + u * kAdamBlock;
+        if (b0 >= t.n) return;
+        const long long i = b0 + 4 * lane;
+        float m[4], v[4];
+        if (t.bits == 8) {
+            const int have = (int)min(t.n - i, 4LL);
+            Piece<int8_t, 4> mc;
+            Piece<uint8_t, 4> vc;
+            mc.load_some(static_cast<const int8_t *>(t.m) + i, have);
+            vc.load_some(static_cast<const uint8_t *>(t.v) + i, have);
+            decode_moments(mc.e, vc.e, t.ms[b0 / kAdamBlock], t.vs[b0 / kAdamBlock], m, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = mul_f32(v[e], v[e]);
+        } else {
+            load4(t.m, PROM_F32, i, t.n, m);
+            load4(t.v, PROM_F32, i, t.n, v);
+        }
+        store4(mo, PROM_F32, i, t.n, m);
+        store4(vo, PROM_F32, i, t.n, v);
+    }
+}
+
+// Table: [count] AdamTensor, then [chunks] int32 owners.
+static long long adam_chunks(const prom_adamw_tensor_t *t, int count)
+{
+    long long c = 0;
+    for (int i = 0; i < count; ++i) c += (t[i].n + kAdamChunk - 1) / kAdamChunk;
+    return c;
+}
+
+static int adam_check(const prom_adamw_tensor_t *t, int count, int *bad)
+{
+    if (bad) *bad = -1;
+    if (!t || count <= 0) return PROM_EINVAL;
+    for (int i = 0; i < count; ++i) {
+        if (bad) *bad = i;
+        const prom_adamw_tensor_t &a = t[i];
+        const int pb = type_bytes(a.param_type), gb = type_bytes(a.grad_type), cb = a.copy ? type_bytes(a.copy_type) : 4;
+        if (!a.param || !a.grad || !a.exp_avg || !a.exp_avg_sq || a.n <= 0 || !pb || !gb || !cb) return PROM_EINVAL;
+        if (a.state_bits != 8 && a.state_bits != 32) return PROM_EINVAL;
+        if (a.state_bits == 8 && (!a.avg_scale || !a.sq_scale)) return PROM_EINVAL;
+        const int sb = a.state_bits / 8;
+        if (misaligned(a.param, pb) || misaligned(a.grad, gb) || misaligned(a.copy, cb) || misaligned(a.exp_avg, sb) || misaligned(a.exp_avg_sq, sb))
+            return PROM_EINVAL;
+        if (misaligned(a.avg_scale, 4) || misaligned(a.sq_scale, 4)) return PROM_EINVAL;
+        if (a.n > (1LL << 42)) return PROM_EUNSUPPORTED;
+        const size_t n = (size_t)a.n, blocks = a.state_bits == 8 ? (n + kAdamBlock - 1) / kAdamBlock * 4 : 0;
+        const Range out[6] = {{a.param, n * pb}, {a.exp_avg, n * sb}, {a.exp_avg_sq, n * sb}, {a.copy, n * cb}, {blocks ? a.avg_scale : nullptr, blocks}, {blocks ? a.sq_scale : nullptr, blocks}};
+        const Range in[1] = {{a.grad, n * gb}};
+        if (outputs_meet(out, 6, in, 1)) return PROM_EALIAS;
+    }
+    if (bad) *bad = -1;
+    if (adam_chunks(t, count) > 0x7fffffffLL) return PROM_EUNSUPPORTED;
+    return PROM_OK;
+}
+
+}  // namespace prom
+
+extern "C" size_t prom_adamw_table_size(const prom_adamw_tensor_t *tensors, int count)
+{
+    using namespace prom;
+    if (adam_check(tensors, count, nullptr) != PROM_OK) return 0;
+    return sizeof(AdamTensor) * (size_t)count + 4 * (size_t)adam_chunks(tensors, count);
+}
+
+extern "C" int prom_adamw_table(const prom_adamw_tensor_t *tensors, int count, void *table_host, size_t table_bytes, prom_adamw_plan_t *plan,
+                                int *bad_tensor)
+{
+    using namespace prom;
+    if (const int rc = adam_check(tensors, count, bad_tensor)) return rc;
+    if (!table_host || !plan) return PROM_EINVAL;
+    const long long chunks = adam_chunks(tensors, count);
+    if (table_bytes < sizeof(AdamTensor) * (size_t)count + 4 * (size_t)chunks) return PROM_EWORKSPACE;
+    unsigned char *out = static_cast<unsigned char *>(table_host);
+    unsigned char *owner = out + sizeof(AdamTensor) * (size_t)count;
+    long long first = 0;
+    for (int i = 0; i < count; ++i) {
+        const prom_adamw_tensor_t &a = tensors[i];
+        const AdamTensor t{a.param, a.grad, a.exp_avg, a.exp_avg_sq, a.avg_scale, a.sq_scale, a.copy, a.n, (int)first,
+                           (int8_t)a.param_type, (int8_t)a.grad_type, (int8_t)a.copy_type, (int8_t)a.state_bits};
+        std::memcpy(out + sizeof(AdamTensor) * (size_t)i, &t, sizeof t);
+        const long long c = (a.n + kAdamChunk - 1) / kAdamChunk;
+        for (long long k = 0; k < c; ++k) std::memcpy(owner + 4 * (size_t)(first + k), &i, 4);
+        first += c;
+    }
+    plan->tensors = count;
+    plan->workgroups = (int32_t)chunks;
+    return PROM_OK;
+}
+
+extern "C" int prom_adamw_step(const void *table, const prom_adamw_plan_t *plan, const prom_adamw_hyper_t *h, void *stream)
+{
+    using namespace prom;
+    if (!table || !plan || !h || plan->tensors <= 0 || plan->workgroups <= 0 || misaligned(table, 8)) return PROM_EINVAL;
+    if (misaligned(h->step_dev, 4) || misaligned(h->lr_dev, 4) || misaligned(h->grad_scale, 4)) return PROM_EINVAL;
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0 && h->eps >= 0.0 && h->weight_decay >= 0.0)) return PROM_EINVAL;
+    if (!h->step_dev && h->step < 1) return PROM_EINVAL;
+    if (!h->lr_dev && !(h->lr >= 0.0)) return PROM_EINVAL;
+    AdamHyper a{};
+    a.beta1 = (float)h->beta1;
+    a.omb1 = (float)(1.0 - h->beta1);
+    a.beta2 = (float)h->beta2;
+    a.omb2 = (float)(1.0 - h->beta2);
+    a.eps = (float)h->eps;
+    a.step = h->step_dev;
+    a.lr = h->lr_dev;
+    a.grad_scale = h->grad_scale;
+    a.lr_h = h->lr;
+    a.wd = h->weight_decay;
+    a.b1 = h->beta1;
+    a.b2 = h->beta2;
+    a.step_h = h->step;
+    if (!a.step && !a.lr) corrections(h->lr, h->weight_decay, h->beta1, h->beta2, h->step, &a.decay, &a.step_size, &a.inv_root2);
+    const AdamTensor *t = static_cast<const AdamTensor *>(table);
+    clear_hip_error();
+    hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)plan->workgroups), dim3(256), 0, static_cast<hipStream_t>(stream), t,
+                       reinterpret_cast<const int *>(t + plan->tensors), a);
+    return check_launch();
+}
+
+extern "C" int prom_adamw_moments(const void *table, const prom_adamw_plan_t *plan, float *const *exp_avg, float *const *exp_avg_sq, void *stream)
+{
+    using namespace prom;
+    if (!table || !plan || plan->tensors <= 0 || plan->workgroups <= 0 || misaligned(table, 8)) return PROM_EINVAL;
+    if (!exp_avg || !exp_avg_sq || misaligned(exp_avg, 8) || misaligned(exp_avg_sq, 8)) return PROM_EINVAL;
+    const AdamTensor *t = static_cast<const AdamTensor *>(table);
+    clear_hip_error();
+    hipLaunchKernelGGL(adamw_moments_kernel, dim3((unsigned)plan->workgroups), dim3(256), 0, static_cast<hipStream_t>(stream), t,
+                       reinterpret_cast<const int *>(t + plan->tensors), exp_avg, exp_avg_sq);
+    return check_launch();
+}

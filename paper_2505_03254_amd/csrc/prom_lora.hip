@@ -1,0 +1,673 @@
+// Ternary pointwise layer with low-rank adapters of many requests, forward and backward: the products with the adapters,
+// the gradients of the adapters, and the entry points.  The product with the shared weights is prom_lora_gemm.hip.
+#include "prom_lora.h"
+#include "prom_launch.h"
+#include "prom_lora_gemm.h"
+
+#include <type_traits>
+
+namespace prom {
+
+// ---- rows by adapter -------------------------------------------------------------------------------------
+// One workgroup per adapter (and one for the elements without): it counts the elements of lower adapters and its own,
+// then writes its own in their order.  Nothing has to wait for another workgroup, and the order is the same every time.
+// Tile k of an adapter whose rows start at position p has the number p / tile + adapter + k: numbers of different adapters
+// never meet, since floor(a) + floor(b) + 1 >= floor(a) + ceil(b), and the unused ones are written as empty.
+__global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__ index, int n, int hw, int adapters, LoraPlan p)
+{
+    __shared__ int eq_of[16], lt_of[16];
+    const int l = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per = ((n + 15) / 16 + 3) & ~3;
+    const int from = min(n, wave * per), to = min(n, from + per);
+    auto group = [&](int id) { return id >= 0 && id < adapters ? id : adapters; };
+    int eq = 0, lt = 0;
+    for (int i = from; i < to; i += 256) {
+        const int have = to - (i + 4 * lane);
+        Piece<int, 4> v;
+        v.load_some(index + i + 4 * lane, have);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int g = group(v.e[e]);
+            eq += __popcll(__ballot(e < have && g == l));
+            lt += __popcll(__ballot(e < have && g < l));
+        }
+    }
+    if (lane == 0) {
+        eq_of[wave] = eq;
+        lt_of[wave] = lt;
+    }
+    __syncthreads();
+    int before = 0, total = 0, lower = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) before += eq_of[w];
+        total += eq_of[w];
+        lower += lt_of[w];
+    }
+    int at = lower + before;
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int i = from; i < to; i += 256) {
+        const int have = to - (i + 4 * lane);
+        Piece<int, 4> v;
+        v.load_some(index + i + 4 * lane, have);
+        unsigned long long b[4];
+        int mine = at, all = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            b[e] = __ballot(e < have && group(v.e[e]) == l);
+            mine += __popcll(b[e] & below);
+            all += __popcll(b[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (b[e] >> lane & 1) p.order[mine++] = i + 4 * lane + e;
+        at += all;
+    }
+    const int first = lower * hw, count = total * hw;
+    if (threadIdx.x == 0) p.groups[l] = int2{first, count};
+    auto cut = [&](int4 *out, int tile) {
+        const int base = first / tile + l, end = (first + count) / tile + l + 1;
+        for (int k = threadIdx.x; k < end - base; k += 1024) out[base + k] = int4{l, first + k * tile, max(0, min(tile, count - k * tile)), 0};
+    };
+    cut(p.tiles, kLoraTile);
+    if (p.chunks) cut(p.chunks, p.chunk);
+}
+
+// ---- the shrinking product: rows of one adapter to `rank` numbers each -------------------------------------
+// A workgroup takes up to 32 sorted rows of one adapter; its 8 wavefronts share the channels in steps (64 of int8, 32 of
+// real input), every one with all of the rows and ranks, and their sums meet in LDS.  Bound by the activations' bytes and,
+// from rank 32 on, by the adapter's, which every workgroup reads from L2.  The backward form writes the activations of the next
+// product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as +-2 there), so that dy is read once for both.
+struct LoraShrinkArgs {
+    const void *in;     // int8 x [m][K] or dy [m][K]
+    const void *low;    // [adapters][rank][K]
+    const int *order;
+    const int4 *tiles;
+    const float *step;  // [n]
+    const float *scale; // [adapters] (backward)
+    const float *w_scale;
+    float *out;         // [m][rank]
+    float *out_step;    // backward: out * step [m][rank]
+    int *rows;          // [m], written
+    bf16_t *planes;     // backward: [m positions][P][Kp] or NULL
+    int hw, K, Kp, rank, adapters;
+};
+
+// eight bf16 of eight int8 codes (exact: 8 significant bits)
+__device__ __forceinline__ v8bf codes_to_bf16(const int8_t *c)
+{
+    v8bf r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (bf16_t)(float)c[e];
+    return r;
+}
+
+template <bool BACK, typename TX, typename TA, int RT>
+__global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a)
+{
+    constexpr int PA = planes_of<TA>();
+    constexpr int PX = BACK ? planes_of<TX>() : 1;
+    constexpr int KS = BACK ? 32 : 64;  // channels of a step
+    constexpr int KL = KS / 4;          // of them a lane's
+    __shared__ v4f red[4][2 * RT][64];
+    const int4 tile = a.tiles[blockIdx.x];
+    const int l = tile.x, count = tile.z;
+    if (count == 0) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j = lane & 15, g = lane >> 4;
+    const bool has = l < a.adapters;
+    const int K = a.K;
+
+    int row[2], elem[2];
+    bool in[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        in[i] = 16 * i + j < count;
+        const int pos = tile.y + min(16 * i + j, count - 1);
+        const int e = pos / a.hw;
+        elem[i] = a.order[e];
+        row[i] = elem[i] * a.hw + (pos - e * a.hw);
+        if (wave == 0 && g == 0 && in[i]) a.rows[pos] = row[i];
+    }
+    v4f acc[2][RT];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[i][t] = v4f{0, 0, 0, 0};
+
+    const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * K;
+    const int limit = BACK && a.planes ? a.Kp : K;
+    for (int k = KS * wave; k < limit && (BACK || has); k += KS * 8) {
+        const int k0 = k + KL * g;
+        v8bf bx[2][BACK ? PX : 2];
+        if constexpr (BACK) {
+            Piece<TX, 8> v[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, K - k0);
+            if (a.planes) {
+                Piece<float, 8> ws;
+                ws.load_some(a.w_scale + k0, K - k0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Piece<bf16_t, 8> o[PX];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        bf16_t s[PX];
+                        split<PX>((float)v[i].e[e] * ws.e[e] * 0.5f, s);
+                        // (the decoded codes come in the order 0, 2, 1, 3 of every four)
+                        constexpr int to[8] = {0, 2, 1, 3, 4, 6, 5, 7};
+#pragma unroll
+                        for (int p = 0; p < PX; ++p) o[p].e[to[e]] = s[p];
+                    }
+                    const size_t pos = (size_t)(tile.y + 16 * i + j);
+                    if (in[i])
+#pragma unroll
+                        for (int p = 0; p < PX; ++p) o[p].store(a.planes + (pos * PX + p) * a.Kp + k0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) split_piece<PX>(v[i], bx[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                Piece<int8_t, 16> v;
+                v.load_some(static_cast<const int8_t *>(a.in) + (size_t)row[i] * K + k0, K - k0);
+                bx[i][0] = codes_to_bf16(v.e);
+                bx[i][1] = codes_to_bf16(v.e + 8);
+            }
+        }
+        if (has) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const int r = min(16 * t + j, a.rank - 1);  // (ranks past the last one repeat it and are not written)
+#pragma unroll
+                for (int h = 0; h < KL / 8; ++h) {
+                    Piece<TA, 8> w;
+                    w.load_some(low + (size_t)r * K + k0 + 8 * h, K - k0 - 8 * h);
+                    v8bf aw[PA];
+                    split_piece<PA>(w, aw);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if constexpr (BACK) {
+#pragma unroll
+                            for (int p = 0; p < PA; ++p)
+#pragma unroll
+                                for (int q = 0; q < PX; ++q)
+                                    if (p + q < 3) acc[i][t] = mfma_bf16(aw[p], bx[i][q], acc[i][t]);
+                        } else {
+#pragma unroll
+                            for (int p = 0; p < PA; ++p) acc[i][t] = mfma_bf16(aw[p], bx[i][h], acc[i][t]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    // sums of the 8 wavefronts, always added in the same order
+    if (wave >= 4)
+#pragma unroll
+        for (int c = 0; c < 2 * RT; ++c) red[wave - 4][c][lane] = acc[c & 1][c >> 1];
+    __syncthreads();
+    if (wave < 4)
+#pragma unroll
+        for (int c = 0; c < 2 * RT; ++c) {
+            const v4f o = red[wave][c][lane];
+            red[wave][c][lane] = acc[c & 1][c >> 1] + o;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int c0 = 0; c0 < 2 * RT; c0 += 8) {
+        const int c = c0 + wave;
+        if (c >= 2 * RT) break;
+        const v4f s = (red[0][c][lane] + red[1][c][lane]) + (red[2][c][lane] + red[3][c][lane]);
+        const int i = c & 1, t = c >> 1;
+        const bool ok = i ? in[1] : in[0];
+        const int r0 = i ? row[1] : row[0];
+        const float step = a.step[i ? elem[1] : elem[0]];
+        const float f = !has ? 0.0f : BACK ? a.scale[l] : step;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 16 * t + 4 * g + e;
+            if (ok && r < a.rank) {
+                const float v = has ? s[e] * f : 0.0f;
+                a.out[(size_t)r0 * a.rank + r] = v;
+                if (BACK && a.out_step) a.out_step[(size_t)r0 * a.rank + r] = v * step;
+            }
+        }
+    }
+}
+
+// The same for a few rows, without sorting: a wavefront per row and RC ranks, the channels over its lanes, float32 on the vector
+// ALU.  Every row reads its own adapter; what bounds it is the latency of two dependent loads and, with many rows, the adapters' bytes.
+template <typename TA, int RC>
+__global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__restrict__ x, const TA *__restrict__ low, const int *__restrict__ index,
+                                                                const float *__restrict__ step, float *__restrict__ hid, int m, int hw, int K,
+                                                                int rank, int adapters)
+{
+    const int lane = threadIdx.x & 63;
+    const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int per = (rank + RC - 1) / RC;
+    const int row = unit / per, r0 = (unit - row * per) * RC;
+    if (row >= m) return;
+    const int l = index[row / hw];
+    const bool has = l >= 0 && l < adapters;
+    float s[RC];
+#pragma unroll
+    for (int c = 0; c < RC; ++c) s[c] = 0.0f;
+    if (has) {
+        const int8_t *xr = x + (size_t)row * K;
+        const TA *lr = low + ((size_t)l * rank + r0) * K;
+#pragma unroll 4
+        for (int k = 8 * lane; k < K; k += 512) {
+            Piece<int8_t, 8> v;
+            v.load_some(xr + k, K - k);
+            Piece<TA, 8> w[RC];
+#pragma unroll
+            for (int c = 0; c < RC; ++c) w[c].load_some(lr + (size_t)(r0 + c < rank ? c : 0) * K + k, K - k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int c = 0; c < RC; ++c) s[c] += (float)v.e[e] * (float)w[c].e[e];
+        }
+    }
+    const float f = step[row / hw];
+#pragma unroll
+    for (int c = 0; c < RC; ++c) {
+        const float t = wave_sum_f32(s[c]);
+        if (lane == 0 && r0 + c < rank) hid[(size_t)row * rank + r0 + c] = has ? t * f : 0.0f;
+    }
+}
+
+// ---- gradients of the adapters ------------------------------------------------------------------------------
+// out_l [rank][C] = sum over the rows of adapter l of coef [row][rank]^T times in [row][C]: both operands of the matrix
+// instruction run along the rows, across the memory's order.  A lane loads 8 rows x 8 neighbouring columns and turns them in
+// its own registers (pairs of rows by v_perm); it then holds 8 rows of its 8 columns, which is one operand for each of
+// 8 tiles whose 16 columns lie 8 apart: no LDS, whole runs of 8 bytes (int8) or 16 to 32 a lane.  A workgroup takes 512 columns and a chunk
+// of one adapter's sorted rows, and writes partial sums; a second kernel adds an adapter's chunks in their order.
+struct LoraGradArgs {
+    const void *in;      // [m][C]
+    const float *coef;   // [m][rank]
+    const float *scale;  // [adapters] or NULL: factor of the coefficients
+    const int *rows;
+    const int4 *chunks;
+    float *part;         // [chunks][rank][C]
+    int C, rank, adapters;
+};
+
+template <typename TX, int RT>
+__global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
+{
+    constexpr bool CODES = std::is_same<TX, int8_t>::value;
+    constexpr int PX = CODES ? 1 : planes_of<TX>();
+    const int4 chunk = a.chunks[blockIdx.x];
+    if (chunk.z == 0 || chunk.x >= a.adapters) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j = lane & 15, g = lane >> 4;
+    const int c0 = (blockIdx.y * 4 + wave) * 128 + 8 * j;
+    const int r0 = blockIdx.z * 16 * RT;
+    if ((int)(blockIdx.y * 4 + wave) * 128 >= a.C) return;
+    const float f = a.scale ? a.scale[chunk.x] : 1.0f;
+
+    v4f acc[RT][8];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[t][e] = v4f{0, 0, 0, 0};
+
+    for (int m = 0; m < chunk.z; m += 32) {
+        const int have = chunk.z - m - 8 * g;  // rows of this lane
+        Piece<int, 8> row;
+        row.load_some(a.rows + chunk.y + m + 8 * g, have);
+        Piece<TX, 8> v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e].load_some(static_cast<const TX *>(a.in) + (size_t)row.e[e] * a.C + c0, e < have ? a.C - c0 : 0);
+        v8bf co[RT][3];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int r = min(r0 + 16 * t + j, a.rank - 1);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float c = e < have ? a.coef[(size_t)row.e[e] * a.rank + r] * f : 0.0f;
+                bf16_t s[3];
+                split<3>(c, s);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) co[t][p][e] = s[p];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            v8bf b[PX];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (CODES) b[0][e] = (bf16_t)(float)v[e].e[c];
+                else {
+                    bf16_t s[PX];
+                    split<PX>((float)v[e].e[c], s);
+#pragma unroll
+                    for (int p = 0; p < PX; ++p) b[p][e] = s[p];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+#pragma unroll
+                    for (int q = 0; q < PX; ++q)
+                        if (p + q < 3) acc[t][c] = mfma_bf16(co[t][p], b[q], acc[t][c]);
+        }
+    }
+    // lane (j, g), register e of tile (t, c): rank 16t + 4g + e, column c0 + c
+    float *out = a.part + (size_t)blockIdx.x * a.rank * a.C;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + 16 * t + 4 * g + e;
+            if (r >= a.rank) continue;
+            Piece<float, 8> o;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o.e[c] = acc[t][c][e];
+            o.store_some(out + (size_t)r * a.C + c0, a.C - c0);
+        }
+}
+
+__global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float *__restrict__ part, const int2 *__restrict__ groups, float *__restrict__ out,
+                                                            int chunk, int rank, int C)
+{
+    const int l = blockIdx.x / rank, r = blockIdx.x - l * rank;
+    const int c0 = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (c0 >= C) return;
+    const int2 grp = groups[l];
+    const int base = grp.x / chunk + l, chunks = (grp.y + chunk - 1) / chunk;
+    Piece<float, 4> s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s.e[e] = 0.0f;
+    for (int k = 0; k < chunks; ++k) {
+        Piece<float, 4> v;
+        v.load_some(part + ((size_t)(base + k) * rank + r) * C + c0, C - c0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s.e[e] += v.e[e];
+    }
+    s.store_some(out + ((size_t)l * rank + r) * C + c0, C - c0);
+}
+
+// ---- host -------------------------------------------------------------------------------------------------
+static size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+// Rows of a chunk of the adapters' gradients: partial sums cost rank * (cin + cout) * 4 bytes a chunk, the chunks of all columns
+// have to fill the chip; 256 rows give 8192 rows 32 chunks of 16 workgroups and more.
+constexpr int kLoraChunk = 256;
+
+struct LoraSpace {  // offsets into the workspace
+    size_t order, rows, groups, tiles, chunks, hid, g, gs, planes, part_a, part_b, bytes;
+    int ntiles, nchunks;
+};
+static LoraSpace lora_space(long long m, int n, int cin, int cout, int adapters, int rank, bool back, int planes)
+{
+    LoraSpace s{};
+    size_t at = 0;
+    auto take = [&](size_t b) {
+        const size_t o = at;
+        at += up256(b);
+        return o;
+    };
+    s.ntiles = (int)(m / kLoraTile) + adapters + 1;
+    s.nchunks = (int)(m / kLoraChunk) + adapters + 1;
+    s.order = take((size_t)n * 4);
+    s.rows = take((size_t)m * 4);
+    s.groups = take((size_t)(adapters + 1) * 8);
+    s.tiles = take((size_t)s.ntiles * 16);
+    if (back) {
+        s.chunks = take((size_t)s.nchunks * 16);
+        s.g = take((size_t)m * rank * 4);
+        s.gs = take((size_t)m * rank * 4);
+        s.planes = take((size_t)m * planes * lora_padded(cout) * 2);
+        s.part_a = take((size_t)s.nchunks * rank * cin * 4);
+        s.part_b = take((size_t)s.nchunks * rank * cout * 4);
+    } else
+        s.hid = take((size_t)m * rank * 4);
+    s.bytes = at;
+    return s;
+}
+
+static int lora_check(int n, int h, int w, int cin, int cout, const void *wq, const prom_lora_t *lo, long long *m)
+{
+    if (!lo || !wq || n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0) return PROM_EINVAL;
+    if (!lo->a || !lo->b || !lo->scale || !lo->index || lo->adapters <= 0 || lo->rank <= 0) return PROM_EINVAL;
+    if (lo->type != PROM_BF16 && lo->type != PROM_F16) return PROM_EINVAL;
+    if (misaligned(wq, 4) || misaligned(lo->a, 2) || misaligned(lo->b, 2) || misaligned(lo->scale, 4) || misaligned(lo->index, 4)) return PROM_EINVAL;
+    if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || lo->rank > kLoraMaxRank || lo->adapters > kLoraMaxAdapters) return PROM_EUNSUPPORTED;
+    const long long hw = (long long)h * w;
+    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return PROM_EUNSUPPORTED;
+    *m = hw * n;
+    return PROM_OK;
+}
+
+template <typename F> static void by_adapter_type(int type, F f)
+{
+    if (type == PROM_BF16) f(bf16_t{});
+    else f(f16_t{});
+}
+template <typename F> static void by_real_type(int type, F f)
+{
+    if (type == PROM_F32) f(float{});
+    else by_adapter_type(type, f);
+}
+// f(rank tiles of 16) up to `most`
+template <typename F> static void by_rank(int rank, F f)
+{
+    if (rank <= 16) f(std::integral_constant<int, 1>{});
+    else if (rank <= 32) f(std::integral_constant<int, 2>{});
+    else if (rank <= 64) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 8>{});
+}
+
+// Up to this many rows run without sorting, on the kernels whose workgroups hold every row.
+constexpr int kLoraFew = 64;
+
+static int planes_of_type(int type) { return type == PROM_F32 ? 3 : type == PROM_F16 ? 2 : 1; }
+
+}  // namespace prom
+
+extern "C" size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank)
+{
+    using namespace prom;
+    if (n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0 || adapters <= 0 || rank <= 0) return 0;
+    if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || rank > kLoraMaxRank || adapters > kLoraMaxAdapters) return 0;
+    const long long hw = (long long)h * w;
+    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return 0;
+    return lora_space(hw * n, n, cin, cout, adapters, rank, false, 0).bytes;
+}
+
+extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, const void *w_packed, int cout, const float *x_step,
+                                 const float *w_scale, const float *bias, const prom_lora_t *lora, void *y, int y_type, float *hid, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    using namespace prom;
+    long long m = 0;
+    if (const int rc = lora_check(n, h, w, cin, cout, w_packed, lora, &m)) return rc;
+    if (!x || !x_step || !w_scale || !y || (y_type != PROM_F32 && y_type != lora->type)) return PROM_EINVAL;
+    const int yb = type_bytes(y_type);
+    if (misaligned(x_step, 4) || misaligned(w_scale, 4) || misaligned(bias, 4) || misaligned(y, yb) || misaligned(hid, 4)) return PROM_EINVAL;
+    const LoraSpace s = lora_space(m, n, cin, cout, lora->adapters, lora->rank, false, 0);
+    if (!workspace || workspace_bytes < s.bytes || misaligned(workspace, 256)) return PROM_EWORKSPACE;
+    const size_t pool = (size_t)lora->adapters * lora->rank * 2;
+    const Range out[3] = {{y, (size_t)m * cout * yb}, {hid, (size_t)m * lora->rank * 4}, {workspace, s.bytes}};
+    const Range in[9] = {{x, (size_t)m * cin}, {w_packed, prom_packed_size(cout, cin)}, {x_step, (size_t)n * 4}, {w_scale, (size_t)cout * 4},
+                         {bias, (size_t)cout * 4}, {lora->a, pool * cin}, {lora->b, pool * cout}, {lora->scale, (size_t)lora->adapters * 4},
+                         {lora->index, (size_t)n * 4}};
+    if (outputs_meet(out, 3, in, 9)) return PROM_EALIAS;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    if (!hid) hid = reinterpret_cast<float *>(ws + s.hid);
+    LoraGemmArgs ga{};
+    ga.x = x;
+    ga.wq = static_cast<const uint32_t *>(w_packed);
+    ga.index = lora->index;
+    ga.step = x_step;
+    ga.w_scale = w_scale;
+    ga.bias = bias;
+    ga.hid = hid;
+    ga.scale = lora->scale;
+    ga.low = lora->b;
+    ga.y = y;
+    ga.m = (int)m;
+    ga.hw = h * w;
+    ga.K = cin;
+    ga.KW = (cin + 15) / 16;
+    ga.Nc = cout;
+    ga.rank = lora->rank;
+    ga.adapters = lora->adapters;
+    clear_hip_error();
+    if (m <= kLoraFew) {
+        by_adapter_type(lora->type, [&](auto t) {
+            using T = decltype(t);
+            auto go = [&](auto rc) {
+                constexpr int RC = decltype(rc)::value;
+                const long long units = m * ((lora->rank + RC - 1) / RC);
+                hipLaunchKernelGGL((lora_shrink_small_kernel<T, RC>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, x, static_cast<const T *>(lora->a),
+                                   lora->index, x_step, hid, (int)m, ga.hw, cin, lora->rank, lora->adapters);
+            };
+            // a rank per wavefront while that leaves SIMDs idle, four (which share the row's codes) from then on
+            if (m * lora->rank <= 1024) go(std::integral_constant<int, 1>{});
+            else go(std::integral_constant<int, 4>{});
+        });
+        lora_gemm_few(ga, lora->type, y_type, st);
+        return check_launch();
+    }
+    LoraPlan p{};
+    p.order = reinterpret_cast<int *>(ws + s.order);
+    p.rows = reinterpret_cast<int *>(ws + s.rows);
+    p.groups = reinterpret_cast<int2 *>(ws + s.groups);
+    p.tiles = reinterpret_cast<int4 *>(ws + s.tiles);
+    hipLaunchKernelGGL(lora_plan_kernel, dim3((unsigned)lora->adapters + 1), dim3(1024), 0, st, lora->index, n, ga.hw, lora->adapters, p);
+    LoraShrinkArgs sa{};
+    sa.in = x;
+    sa.low = lora->a;
+    sa.order = p.order;
+    sa.tiles = p.tiles;
+    sa.step = x_step;
+    sa.out = hid;
+    sa.rows = p.rows;
+    sa.hw = ga.hw;
+    sa.K = cin;
+    sa.rank = lora->rank;
+    sa.adapters = lora->adapters;
+    by_adapter_type(lora->type, [&](auto t) {
+        by_rank(lora->rank, [&](auto rt) {
+            hipLaunchKernelGGL((lora_shrink_kernel<false, float, decltype(t), decltype(rt)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
+        });
+    });
+    ga.rows = p.rows;
+    lora_gemm(ga, lora->type, y_type, false, st);
+    return check_launch();
+}
+
+extern "C" size_t prom_pw_conv_lora_backward_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank, int dy_type)
+{
+    using namespace prom;
+    if (prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank) == 0 || !type_bytes(dy_type)) return 0;
+    return lora_space((long long)n * h * w, n, cin, cout, adapters, rank, true, planes_of_type(dy_type)).bytes;
+}
+
+extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int8_t *x, int n, int h, int w, int cin, const void *wt_packed, int cout,
+                                          const float *x_step, const float *w_scale, const prom_lora_t *lora, const float *hid, void *dx, float *da,
+                                          float *db, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace prom;
+    long long m = 0;
+    if (const int rc = lora_check(n, h, w, cin, cout, dx ? wt_packed : static_cast<const void *>(dy), lora, &m)) return rc;
+    if (!dy || !x_step || (!dx && !da && !db) || (dx && !w_scale) || (da && !x) || (db && !hid)) return PROM_EINVAL;
+    if (dy_type != PROM_F32 && dy_type != lora->type) return PROM_EINVAL;
+    const int yb = type_bytes(dy_type), planes = planes_of_type(dy_type);
+    if (misaligned(dy, yb) || misaligned(dx, yb) || misaligned(x_step, 4) || misaligned(w_scale, 4) || misaligned(hid, 4) || misaligned(da, 4) || misaligned(db, 4))
+        return PROM_EINVAL;
+    const LoraSpace s = lora_space(m, n, cin, cout, lora->adapters, lora->rank, true, planes);
+    if (!workspace || workspace_bytes < s.bytes || misaligned(workspace, 256)) return PROM_EWORKSPACE;
+    const size_t pool = (size_t)lora->adapters * lora->rank;
+    const Range out[4] = {{dx, (size_t)m * cin * yb}, {da, pool * cin * 4}, {db, pool * cout * 4}, {workspace, s.bytes}};
+    const Range in[9] = {{dy, (size_t)m * cout * yb}, {x, (size_t)m * cin}, {dx ? wt_packed : nullptr, prom_packed_size(cin, cout)}, {x_step, (size_t)n * 4},
+                         {w_scale, (size_t)cout * 4}, {lora->a, pool * cin * 2}, {lora->b, pool * cout * 2}, {hid, (size_t)m * lora->rank * 4},
+                         {lora->index, (size_t)n * 4}};
+    const Range more[1] = {{lora->scale, (size_t)lora->adapters * 4}};
+    if (outputs_meet(out, 4, in, 9) || outputs_meet(out, 4, more, 1)) return PROM_EALIAS;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    const int hw = h * w;
+    LoraPlan p{};
+    p.order = reinterpret_cast<int *>(ws + s.order);
+    p.rows = reinterpret_cast<int *>(ws + s.rows);
+    p.groups = reinterpret_cast<int2 *>(ws + s.groups);
+    p.tiles = reinterpret_cast<int4 *>(ws + s.tiles);
+    p.chunks = reinterpret_cast<int4 *>(ws + s.chunks);
+    p.chunk = kLoraChunk;
+    clear_hip_error();
+    hipLaunchKernelGGL(lora_plan_kernel, dim3((unsigned)lora->adapters + 1), dim3(1024), 0, st, lora->index, n, hw, lora->adapters, p);
+    LoraShrinkArgs sa{};
+    sa.in = dy;
+    sa.low = lora->b;
+    sa.order = p.order;
+    sa.tiles = p.tiles;
+    sa.step = x_step;
+    sa.scale = lora->scale;
+    sa.w_scale = w_scale;
+    sa.out = reinterpret_cast<float *>(ws + s.g);
+    sa.out_step = reinterpret_cast<float *>(ws + s.gs);
+    sa.rows = p.rows;
+    sa.planes = dx ? reinterpret_cast<bf16_t *>(ws + s.planes) : nullptr;
+    sa.hw = hw;
+    sa.K = cout;
+    sa.Kp = lora_padded(cout);
+    sa.rank = lora->rank;
+    sa.adapters = lora->adapters;
+    by_adapter_type(lora->type, [&](auto t) {
+        by_rank(lora->rank, [&](auto rt) {
+            const dim3 grid((unsigned)s.ntiles), block(512);
+            if (dy_type == PROM_F32)
+                hipLaunchKernelGGL((lora_shrink_kernel<true, float, decltype(t), decltype(rt)::value>), grid, block, 0, st, sa);
+            else
+                hipLaunchKernelGGL((lora_shrink_kernel<true, decltype(t), decltype(t), decltype(rt)::value>), grid, block, 0, st, sa);
+        });
+    });
+    if (dx) {
+        LoraGemmArgs ga{};
+        ga.x = ws + s.planes;
+        ga.wq = static_cast<const uint32_t *>(wt_packed);
+        ga.rows = p.rows;
+        ga.index = lora->index;
+        ga.hid = sa.out;
+        ga.low = lora->a;
+        ga.y = dx;
+        ga.m = (int)m;
+        ga.hw = hw;
+        ga.K = cout;
+        ga.KW = (cout + 15) / 16;
+        ga.Nc = cin;
+        ga.rank = lora->rank;
+        ga.adapters = lora->adapters;
+        ga.planes = planes;
+        ga.Kp = sa.Kp;
+        lora_gemm(ga, lora->type, dy_type, true, st);
+    }
+    auto grad = [&](const void *in, int in_type, const float *coef, const float *scale, float *part, float *dst, int C) {
+        LoraGradArgs g{in, coef, scale, p.rows, p.chunks, part, C, lora->rank, lora->adapters};
+        auto go = [&](auto t) {
+            const unsigned cols = (unsigned)((C + 511) / 512);
+            if (lora->rank <= 16)
+                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 1>), dim3((unsigned)s.nchunks, cols, 1), dim3(256), 0, st, g);
+            else
+                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 2>), dim3((unsigned)s.nchunks, cols, (unsigned)((lora->rank + 31) / 32)), dim3(256), 0, st, g);
+        };
+        if (in_type < 0) go(int8_t{});
+        else by_real_type(in_type, go);
+        hipLaunchKernelGGL(lora_grad_sum_kernel, dim3((unsigned)(lora->adapters * lora->rank), (unsigned)((C + 1023) / 1024)), dim3(256), 0, st, part, p.groups,
+                           dst, kLoraChunk, lora->rank, C);
+    };
+    if (da) grad(x, -1, sa.out_step, nullptr, reinterpret_cast<float *>(ws + s.part_a), da, cin);
+    if (db) grad(dy, dy_type, hid, lora->scale, reinterpret_cast<float *>(ws + s.part_b), db, cout);
+    return check_launch();
+}

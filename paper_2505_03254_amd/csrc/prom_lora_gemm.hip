@@ -1,0 +1,470 @@
+// y = (rows x ternary weights) scaled, plus the rows' low-rank terms: the product behind prom_pw_conv_lora and, on bf16 planes,
+// the gradient of its activations.
+//
+// Tiled kernel.  As in the kernel of wide layers (prom_pw_gemm.hip) the k loop is outermost over a workgroup's tile, a wavefront owns
+// 16*PT rows x 64 channels, decodes its own packed codes in registers and reads the rows' operands from two LDS slabs, filled a
+// step ahead.  A step is 128 bytes of every row: 128 int8 or 64 bf16, two matrix instructions deep per accumulator, so
+// that a barrier stands against 2*4*PT of them.
+// A code is two's complement in two bits.  At the top of a byte it reads as 0, 64 or -64; at the top of 16 bits as the bf16 0, 2 or
+// -2: decoding is a shift and a mask, 7 instructions for 16 codes in int8 and 15 in bf16.  The sums are 64 (exact in int32)
+// and 2 times too large; the first is shifted back, the second has its half in the input planes.
+// Rows are taken in the order of their adapters, so a wavefront's rows hold few of them: per adapter it loads its channels'
+// factors once and adds hid b with the accumulators as the third operand.  hid goes in as bf16 planes side by side: of
+// the 32 deep instruction 16 ranks take the first plane and 16 the second; a second instruction carries the third plane
+// and the factors' second one where the types have them, a third one the product of both second planes.
+#include "prom_lora_gemm.h"
+#include "prom_device.h"
+#include "prom_launch.h"
+#include "prom_pw_stream.h"
+
+namespace prom {
+
+__device__ __forceinline__ void lora_lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// 16 codes of a word as 64 times their values, in the order of decode_word
+__device__ __forceinline__ v4i decode_word_64(uint32_t w)
+{
+    return v4i{(int)((w << 6) & 0xc0c0c0c0u), (int)((w << 4) & 0xc0c0c0c0u), (int)((w << 2) & 0xc0c0c0c0u), (int)(w & 0xc0c0c0c0u)};
+}
+// 8 codes (H: first or second 8 of the 16) as bf16 of twice their values, channels in the order 0, 2, 1, 3 of every four
+template <int H> __device__ __forceinline__ v8bf decode_half_bf16(uint32_t w)
+{
+    constexpr int d = 2 * H;
+    const v4i r = {(int)((w << (14 - 2 * d)) & 0xc000c000u), (int)((H ? w << 2 : w << 6) & 0xc000c000u),
+                   (int)((w << (12 - 2 * d)) & 0xc000c000u), (int)((H ? w : w << 4) & 0xc000c000u)};
+    return __builtin_bit_cast(v8bf, r);
+}
+
+// (acc * w_scale) * x_step + bias in three float32 operations, as prom_pw_conv_dynq forms it; acc64 is 64 times the sum
+__device__ __forceinline__ float base_value(int acc64, float w_scale, float x_step, float bias)
+{
+    return add_f32(mul_f32(mul_f32((float)(acc64 >> 6), w_scale), x_step), bias);
+}
+
+template <typename TO, typename TA> struct LowPlanes {
+    // one instruction for bf16 factors and 16-bit results (f16 tells 11 bits apart: hid in 16 are enough); two otherwise
+    static constexpr int HID = sizeof(TO) == 4 ? 3 : 2;
+    static constexpr int LOW = planes_of<TA>();
+    static constexpr bool SECOND = HID == 3 || LOW == 2;
+    static constexpr bool THIRD = HID == 3 && LOW == 2;  // the second planes of both
+};
+
+// Operand of hid for ranks 16*rc + 8*(g & 1) + 0..7 of a row: lanes of g < 2 hold the first plane, the others the second; `second`:
+// the first plane again beside the third.
+template <bool SECOND>
+__device__ __forceinline__ void hid_operand(const float *hid, int have, float f, int g, bool mine, v8bf &first, v8bf &second)
+{
+    Piece<float, 8> v;
+    v.load_some(hid, mine ? have : 0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        bf16_t s[3];
+        split<3>(v.e[e] * f, s);
+        first[e] = g < 2 ? s[0] : s[1];
+        if constexpr (SECOND) second[e] = g < 2 ? s[0] : s[2];
+    }
+}
+
+constexpr int kCodeStep = 64 * 16 + 32;  // a wavefront's words of a word step: [64 channels][4 words]
+constexpr int kCodeBytes = 4 * kCodeStep;
+
+template <int PT, int NW> struct LoraGeom {
+    static constexpr int NT = 64 * NW;
+    static constexpr int TM = 16 * PT;
+    static constexpr int TN = 64 * NW;
+    static constexpr int NQ = TM * 8 / NT;  // 16-byte pieces of a step per thread
+    static constexpr int SLAB = TM * 128;
+    static constexpr int OUT = 16 * (64 * 4 + 16);  // a wavefront's 16 rows x 64 channels on their way out (float32 at most)
+    static constexpr int WAVE = kCodeBytes > OUT ? kCodeBytes : OUT;
+    static constexpr size_t LDS = (size_t)2 * SLAB + NW * WAVE;
+};
+
+// PLANES: bf16 planes instead of int8 (aligned and padded by their writer).
+template <int PT, int NW, bool PLANES, typename TO, typename TA>
+__global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArgs a, int ntiles)
+{
+    using G = LoraGeom<PT, NW>;
+    constexpr int NQ = G::NQ;
+    using Acc = typename std::conditional<PLANES, v4f, v4i>::type;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int j = lane & 15, g = lane >> 4;
+    const int lid = logical_block_id();
+    const int mtiles = (a.m + G::TM - 1) / G::TM;
+    const int ntile = lid % ntiles, mtile = lid / ntiles;
+    if (mtile >= mtiles) return;
+    const int n0 = ntile * G::TN + 64 * wave;  // this wavefront's first channel
+    const int m0 = mtile * G::TM;
+    const int K = a.K, KW = a.KW, Nc = a.Nc;
+
+    // ---- rows: piece idx = tid + NT*q of a slab is slot idx & 7 of row idx >> 3 and holds the row's piece slot ^ (row & 7)
+    const int row_bytes = PLANES ? a.planes * a.Kp * 2 : K;
+    const int piece = (tid & 7) ^ ((tid >> 3) & 7);
+    const unsigned char *src[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const int pos = min(m0 + ((tid + G::NT * q) >> 3), a.m - 1);
+        const int row = PLANES ? pos : a.rows[pos];
+        src[q] = static_cast<const unsigned char *>(a.x) + (size_t)row * row_bytes;
+    }
+    const int steps = (row_bytes + 127) >> 7, whole = row_bytes >> 7;
+    v4i xr[NQ];
+    auto load_x = [&](int s) __attribute__((always_inline)) {
+        const int at = 128 * s + 16 * piece;
+        if (s < whole) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) xr[q] = *reinterpret_cast<const v4i_u *>(src[q] + at);
+        } else {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                Piece<int8_t, 16> v;
+                v.load_some(reinterpret_cast<const int8_t *>(src[q]) + at, row_bytes - at);
+                xr[q] = __builtin_bit_cast(v4i, v);
+            }
+        }
+    };
+    auto put_x = [&](int slab) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) *reinterpret_cast<v4i *>(lds + slab * G::SLAB + (tid + G::NT * q) * 16) = xr[q];
+    };
+
+    // ---- codes: 16 words of each of the wavefront's 64 channels at a time, 4 word steps; instruction r of a load: channel
+    // 16*r + (lane >> 2), word step lane & 3.  A word step is 64 channels of input; planes follow each other.
+    unsigned char *codes = lds + 2 * G::SLAB + wave * G::WAVE;
+    const int wsteps = PLANES ? a.Kp >> 6 : (KW + 3) >> 2;  // of one plane
+    const int wall = PLANES ? wsteps * a.planes : wsteps;
+    const int wpiece = lane & 3;
+    const uint32_t *wrow[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) wrow[r] = a.wq + (size_t)min(n0 + 16 * r + (lane >> 2), Nc - 1) * KW;
+    v4i wr[4];
+    auto load_w = [&](int group) __attribute__((always_inline)) {
+        int ws = 4 * group + wpiece;
+        const bool in = ws < wall;
+        if constexpr (PLANES) {
+            if (ws >= wsteps) ws -= wsteps;
+            if (ws >= wsteps) ws -= wsteps;
+        }
+        const int have = in ? KW - 4 * ws : 0;
+        if (4 * group + 4 <= (KW >> 2)) {  // (every lane's four words lie in the row: also where planes follow each other, for the first)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(wrow[r] + 4 * ws);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Piece<int, 4> v;
+                if (have >= 4) v.load(reinterpret_cast<const int *>(wrow[r] + 4 * ws));
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v.e[e] = e < have ? (int)wrow[r][4 * ws + e] : 0;
+                wr[r] = v4i{v.e[0], v.e[1], v.e[2], v.e[3]};
+            }
+        }
+    };
+    unsigned char *wput = codes + wpiece * kCodeStep + (lane >> 2) * 16;
+    const unsigned char *wget = codes + j * 16 + g * 4;
+    auto put_w = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *reinterpret_cast<v4i *>(wput + 256 * r) = wr[r];
+    };
+
+    Acc acc[PT][4];
+#pragma unroll
+    for (int i = 0; i < PT; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[i][t] = Acc{0, 0, 0, 0};
+
+    load_w(0);
+    load_x(0);
+    put_w();
+    load_w(1);
+    put_x(0);
+    load_x(1 < steps ? 1 : 0);
+    lora_lds_barrier();
+
+    const int sw = (j & 7);
+    constexpr int WS = PLANES ? 1 : 2;   // word steps of a step
+    constexpr int GS = 4 / WS;           // steps of a group of codes
+    for (int s = 0; s < steps; ++s) {
+        const unsigned char *slab = lds + (s & 1) * G::SLAB + j * 128;
+        uint32_t wc[WS][4];
+#pragma unroll
+        for (int h = 0; h < WS; ++h)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) wc[h][t] = *reinterpret_cast<const uint32_t *>(wget + (WS * (s % GS) + h) * kCodeStep + 256 * t);
+        put_x((s + 1) & 1);
+        load_x(s + 2 < steps ? s + 2 : steps - 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v4i B[PT];
+            const int p = PLANES ? 2 * g + h : 4 * h + g;
+#pragma unroll
+            for (int i = 0; i < PT; ++i) B[i] = *reinterpret_cast<const v4i *>(slab + i * 2048 + ((p ^ sw) << 4));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if constexpr (PLANES) {
+                    const v8bf A = h ? decode_half_bf16<1>(wc[0][t]) : decode_half_bf16<0>(wc[0][t]);
+#pragma unroll
+                    for (int i = 0; i < PT; ++i) acc[i][t] = mfma_bf16(A, __builtin_bit_cast(v8bf, B[i]), acc[i][t]);
+                } else {
+                    const v4i A = decode_word_64(wc[h][t]);
+#pragma unroll
+                    for (int i = 0; i < PT; ++i) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, B[i], acc[i][t], 0, 0, 0);
+                }
+            }
+        }
+        if (s % GS == GS - 1) {  // (LDS operations of a wavefront keep their order, and no other one reads these words)
+            put_w();
+            load_w(s / GS + 2);
+        }
+        lora_lds_barrier();
+    }
+
+    // ---- epilogue: lane (j, g), register e of tile (i, t): row 16i + j, channel n0 + 16t + 4g + e --------------------
+    int row[PT], group[PT];
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+        const int pos = m0 + 16 * i + j;
+        row[i] = a.rows[min(pos, a.m - 1)];
+        const int el = a.hw == 1 ? row[i] : row[i] / a.hw;
+        group[i] = a.index[el];
+        if (pos >= a.m || group[i] < 0 || group[i] >= a.adapters) group[i] = 0x7fffffff;
+    }
+    v4f z[PT][4];
+    if constexpr (PLANES) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) z[i][t] = acc[i][t];
+    } else {
+        v4f ws[4], bi[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = min(n0 + 16 * t + 4 * g + e, Nc - 1);
+                ws[t][e] = a.w_scale[c];
+                bi[t][e] = a.bias ? a.bias[c] : 0.0f;
+            }
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const float st = a.step[a.hw == 1 ? row[i] : row[i] / a.hw];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[i][t][e] = base_value(acc[i][t][e], ws[t][e], st, bi[t][e]);
+        }
+    }
+    using L = LowPlanes<TO, TA>;
+    const TA *low = static_cast<const TA *>(a.low);
+    int now = -1;
+    for (;;) {
+        // the wavefront's next adapter: the smallest one above the last
+        int next = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) next = group[i] > now ? min(next, group[i]) : next;
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, 64));
+        now = __builtin_amdgcn_readfirstlane(next);
+        if (now == 0x7fffffff) break;
+        const float f = a.scale ? a.scale[now] : 1.0f;
+        for (int r0 = 0; r0 < a.rank; r0 += 16) {
+            const int rl = r0 + 8 * (g & 1);
+            v8bf A1[4], A2[L::SECOND ? 4 : 1], A3[L::THIRD ? 4 : 1];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int c = min(n0 + 16 * t + j, Nc - 1);
+                TA v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = low[((size_t)now * a.rank + min(rl + e, a.rank - 1)) * Nc + c];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    bf16_t s[L::LOW];
+                    split<L::LOW>(rl + e < a.rank ? (float)v[e] : 0.0f, s);
+                    A1[t][e] = s[0];
+                    if constexpr (L::THIRD) A3[t][e] = g < 2 ? (bf16_t)0.0f : s[1];
+                    if constexpr (L::SECOND) A2[t][e] = g < 2 ? (L::LOW == 2 ? s[L::LOW - 1] : (bf16_t)0.0f) : s[0];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < PT; ++i) {
+                const bool mine = group[i] == now;
+                const unsigned long long here = __ballot(mine);
+                if (here == 0) continue;
+                v8bf b1, b2;
+                hid_operand<L::SECOND>(a.hid + (size_t)row[i] * a.rank + rl, a.rank - rl, f, g, mine, b1, b2);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    v4f v = mfma_bf16(A1[t], b1, z[i][t]);
+                    if constexpr (L::SECOND) v = mfma_bf16(A2[t], b2, v);
+                    if constexpr (L::THIRD) v = mfma_bf16(A3[t], b1, v);
+                    if (here == ~0ull) z[i][t] = v;
+                    else  // (zeros in the others' place would not keep an infinity of this adapter from their rows)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[i][t][e] = mine ? v[e] : z[i][t][e];
+                }
+            }
+        }
+    }
+    // out through the wavefront's own LDS: 16 rows x 64 channels at a time, rows in whole runs
+    constexpr int PITCH = 64 * (int)sizeof(TO) + 16;
+    constexpr int VE = 16 / sizeof(TO), PR = 64 / VE;  // elements of a piece, pieces of a row
+    TO *y = static_cast<TO *>(a.y);
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            Piece<TO, 4> o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o.e[e] = (TO)z[i][t][e];
+            o.store(reinterpret_cast<TO *>(codes + j * PITCH) + 16 * t + 4 * g);
+        }
+#pragma unroll
+        for (int q = 0; q < 16 * PR / 64; ++q) {
+            const int idx = lane + 64 * q;
+            const int rr = idx / PR, c = idx % PR * VE;
+            Piece<TO, VE> o;
+            o.load(reinterpret_cast<const TO *>(codes + rr * PITCH) + c);
+            const int dst = __shfl(row[i], rr, 64);
+            if (m0 + 16 * i + rr < a.m) o.store_some(y + (size_t)dst * Nc + n0 + c, Nc - n0 - c);
+        }
+    }
+}
+
+// ---- a few rows -----------------------------------------------------------------------------------------------
+// Up to 64 rows: a workgroup owns 16 channels and all rows, its 8 wavefronts share the input channels 256 at a time (16 bytes of
+// codes per lane, 64 channels each), the sums meet in LDS.  The low-rank term is one dot product over the ranks per output on the
+// vector ALU, every row with its own adapter.  Bound by latency, then by the adapters' bytes.
+template <typename TO, typename TA, int MT>
+__global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a)
+{
+    __shared__ v4i red[8][MT][64];
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int j = lane & 15, g = lane >> 4;
+    const int n0 = logical_block_id() * 16;
+    if (n0 >= a.Nc) return;
+    const int K = a.K, KW = a.KW;
+    const uint32_t *wrow = a.wq + (size_t)min(n0 + j, a.Nc - 1) * KW;
+    v4i acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
+    for (int k = 256 * wave; k < K; k += 2048) {
+        const int k0 = k + 64 * g;
+        const int have = KW - k0 / 16;
+        Piece<int, 4> w;
+        if (have >= 4) w.load(reinterpret_cast<const int *>(wrow + k0 / 16));
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.e[e] = e < have ? (int)wrow[k0 / 16 + e] : 0;
+        Piece<int8_t, 16> v[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[i][q].load_some(static_cast<const int8_t *>(a.x) + (size_t)min(16 * i + j, a.m - 1) * K + k0 + 16 * q, K - k0 - 16 * q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const v4i A = decode_word_64((uint32_t)w.e[q]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[i][q]), acc[i], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
+    __syncthreads();
+    // thread: row tid / 8, channels n0 + 2 * (tid % 8) and the next
+    const int row = tid >> 3, cc = 2 * (tid & 7);
+    if (row >= a.m || row >= 16 * MT) return;
+    int s0 = 0, s1 = 0;
+    {
+        const int i = row >> 4, from = (row & 15) + 16 * (cc >> 2), e = cc & 3;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const int *p = reinterpret_cast<const int *>(&red[w][i][from]) + e;
+            s0 += p[0];
+            s1 += p[1];
+        }
+    }
+    const int c = n0 + cc;
+    if (c >= a.Nc) return;
+    const bool two = c + 1 < a.Nc;
+    const int el = a.hw == 1 ? row : row / a.hw;
+    const float st = a.step[el];
+    float z0 = base_value(s0, a.w_scale[c], st, a.bias ? a.bias[c] : 0.0f);
+    float z1 = two ? base_value(s1, a.w_scale[c + 1], st, a.bias ? a.bias[c + 1] : 0.0f) : 0.0f;
+    const int l = a.index[el];
+    if (l >= 0 && l < a.adapters) {
+        const TA *low = static_cast<const TA *>(a.low) + (size_t)l * a.rank * a.Nc + c;
+        const float *h = a.hid + (size_t)row * a.rank;
+        float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll 8
+        for (int r = 0; r < a.rank; ++r) {
+            Piece<TA, 2> b;
+            b.load_some(low + (size_t)r * a.Nc, two ? 2 : 1);
+            l0 += h[r] * (float)b.e[0];
+            l1 += h[r] * (float)b.e[1];
+        }
+        const float f = a.scale[l];
+        z0 += f * l0;
+        z1 += f * l1;
+    }
+    Piece<TO, 2> o;
+    o.e[0] = (TO)z0;
+    o.e[1] = (TO)z1;
+    o.store_some(static_cast<TO *>(a.y) + (size_t)row * a.Nc + c, two ? 2 : 1);
+}
+
+// ---- launch ----------------------------------------------------------------------------------------------------
+template <int PT, int NW, bool PLANES, typename TO, typename TA> static void gemm_launch(const LoraGemmArgs &a, hipStream_t st)
+{
+    using G = LoraGeom<PT, NW>;
+    const int ntiles = (a.Nc + G::TN - 1) / G::TN;
+    const long long mtiles = (a.m + G::TM - 1) / G::TM;
+    hipLaunchKernelGGL((lora_gemm_kernel<PT, NW, PLANES, TO, TA>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(G::NT), G::LDS, st, a, ntiles);
+}
+
+template <bool PLANES, typename TO, typename TA> static void gemm_pick(const LoraGemmArgs &a, hipStream_t st)
+{
+    // the widest tile that still gives every compute unit a workgroup
+    auto tiles = [&](int tm, int tn) { return (long long)((a.m + tm - 1) / tm) * ((a.Nc + tn - 1) / tn); };
+    if (tiles(128, 256) >= 256) gemm_launch<8, 4, PLANES, TO, TA>(a, st);
+    else if (tiles(64, 128) >= 256) gemm_launch<4, 2, PLANES, TO, TA>(a, st);
+    else gemm_launch<2, 2, PLANES, TO, TA>(a, st);
+}
+
+template <typename F> static void by_types(int adapter_type, int out_type, F f)
+{
+    if (adapter_type == PROM_BF16) {
+        if (out_type == PROM_F32) f(float{}, bf16_t{});
+        else f(bf16_t{}, bf16_t{});
+    } else {
+        if (out_type == PROM_F32) f(float{}, f16_t{});
+        else f(f16_t{}, f16_t{});
+    }
+}
+
+void lora_gemm(const LoraGemmArgs &a, int adapter_type, int out_type, bool planes, hipStream_t st)
+{
+    by_types(adapter_type, out_type, [&](auto to, auto ta) {
+        if (planes) gemm_pick<true, decltype(to), decltype(ta)>(a, st);
+        else gemm_pick<false, decltype(to), decltype(ta)>(a, st);
+    });
+}
+
+void lora_gemm_few(const LoraGemmArgs &a, int adapter_type, int out_type, hipStream_t st)
+{
+    by_types(adapter_type, out_type, [&](auto to, auto ta) {
+        using TO = decltype(to);
+        using TA = decltype(ta);
+        const dim3 grid((unsigned)(((a.Nc + 15) / 16 + 7) / 8 * 8)), block(512);
+        if (a.m <= 16) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1>), grid, block, 0, st, a);
+        else if (a.m <= 32) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 2>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 4>), grid, block, 0, st, a);
+    });
+}
+
+}  // namespace prom

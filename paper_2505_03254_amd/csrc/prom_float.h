@@ -16,6 +16,10 @@ typedef _Float16 f16_t;
 
 inline int type_bytes(int type) { return type == PROM_F32 ? 4 : type == PROM_BF16 || type == PROM_F16 ? 2 : 0; }
 
+// The same pointer, known to point to global memory (one that comes out of memory or of a struct of pointers may be anything
+// to the compiler, and a flat access waits for LDS too).
+template <typename T> __device__ __forceinline__ T *as_global(T *p) { return (T *)(__attribute__((address_space(1))) T *)p; }
+
 // A piece of 16 (8, 4) bytes at an address that is aligned to its elements only: gfx950 loads and stores dwords at any
 // byte address, and the row of an odd width starts anywhere.
 template <typename T, int N> struct Piece {
@@ -124,6 +128,9 @@ __device__ __forceinline__ double wave_sum_f64(double v)
     const int hi = __builtin_amdgcn_readlane((int)(b >> 32), 63);
     return __longlong_as_double(((long long)hi << 32) | (unsigned)lo);
 }
+
+// Workgroup barrier that orders LDS traffic only: loads of global memory stay on their way across it.
+__device__ __forceinline__ void lds_only_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // ---- host ------------------------------------------------------------------------------------
 inline bool misaligned(const void *p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) != 0; }

@@ -19,8 +19,6 @@
 
 namespace prom {
 
-__device__ __forceinline__ void lora_lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
 // 16 codes of a word as 64 times their values, in the order of decode_word
 __device__ __forceinline__ v4i decode_word_64(uint32_t w)
 {
@@ -49,22 +47,7 @@ template <typename TO, typename TA> struct LowPlanes {
     static constexpr bool THIRD = HID == 3 && LOW == 2;  // the second planes of both
 };
 
-// Operand of hid for ranks 16*rc + 8*(g & 1) + 0..7 of a row: lanes of g < 2 hold the first plane, the others the second; `second`:
-// the first plane again beside the third.
-template <bool SECOND>
-__device__ __forceinline__ void hid_operand(const float *hid, int have, float f, int g, bool mine, v8bf &first, v8bf &second)
-{
-    Piece<float, 8> v;
-    v.load_some(hid, mine ? have : 0);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        bf16_t s[3];
-        split<3>(v.e[e] * f, s);
-        first[e] = g < 2 ? s[0] : s[1];
-        if constexpr (SECOND) second[e] = g < 2 ? s[0] : s[2];
-    }
-}
-
+constexpr int kNone = 0x7fffffff;  // the adapter of rows without one
 constexpr int kCodeStep = 64 * 16 + 32;  // a wavefront's words of a word step: [64 channels][4 words]
 constexpr int kCodeBytes = 4 * kCodeStep;
 
@@ -76,7 +59,9 @@ template <int PT, int NW> struct LoraGeom {
     static constexpr int SLAB = TM * 128;
     static constexpr int OUT = 16 * (64 * 4 + 16);  // a wavefront's 16 rows x 64 channels on their way out (float32 at most)
     static constexpr int WAVE = kCodeBytes > OUT ? kCodeBytes : OUT;
-    static constexpr size_t LDS = (size_t)2 * SLAB + NW * WAVE;
+    static constexpr int ROWS = 2 * SLAB + NW * WAVE;       // row, adapter, step of every row
+    static constexpr int CHANS = ROWS + TM * 12;            // w_scale, bias of every channel
+    static constexpr size_t LDS = (size_t)CHANS + TN * 8;
 };
 
 // PLANES: bf16 planes instead of int8 (aligned and padded by their writer).
@@ -109,21 +94,16 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         const int row = PLANES ? pos : a.rows[pos];
         src[q] = static_cast<const unsigned char *>(a.x) + (size_t)row * row_bytes;
     }
-    const int steps = (row_bytes + 127) >> 7, whole = row_bytes >> 7;
+    // Steps in the order they are taken: what is left behind the whole ones comes first, read piece by piece with zeros behind the row's
+    // end, so that everything later loads whole pieces without a test (the order of a sum of integers is free; planes are padded).
+    const int whole = row_bytes >> 7;
+    const int first = !PLANES && (row_bytes & 127) ? 1 : 0;
+    const int steps = whole + first;
     v4i xr[NQ];
-    auto load_x = [&](int s) __attribute__((always_inline)) {
-        const int at = 128 * s + 16 * piece;
-        if (s < whole) {
+    auto load_x = [&](int q) __attribute__((always_inline)) {
+        const int at = 128 * (q - first) + 16 * piece;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) xr[q] = *reinterpret_cast<const v4i_u *>(src[q] + at);
-        } else {
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                Piece<int8_t, 16> v;
-                v.load_some(reinterpret_cast<const int8_t *>(src[q]) + at, row_bytes - at);
-                xr[q] = __builtin_bit_cast(v4i, v);
-            }
-        }
+        for (int i = 0; i < NQ; ++i) xr[i] = *reinterpret_cast<const v4i_u *>(as_global(src[i] + at));
     };
     auto put_x = [&](int slab) __attribute__((always_inline)) {
 #pragma unroll
@@ -131,36 +111,33 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     };
 
     // ---- codes: 16 words of each of the wavefront's 64 channels at a time, 4 word steps; instruction r of a load: channel
-    // 16*r + (lane >> 2), word step lane & 3.  A word step is 64 channels of input; planes follow each other.
+    // 16*r + (lane >> 2), word step lane & 3.  A word step is 64 channels of input; planes follow each other.  Words past a row's end are replaced
+    // by its last one: they meet zeros of the other operand.
+    constexpr int WS = PLANES ? 1 : 2;   // word steps of a step
+    constexpr int GS = 4 / WS;           // steps of a group of codes
     unsigned char *codes = lds + 2 * G::SLAB + wave * G::WAVE;
-    const int wsteps = PLANES ? a.Kp >> 6 : (KW + 3) >> 2;  // of one plane
-    const int wall = PLANES ? wsteps * a.planes : wsteps;
+    const int wsteps = PLANES ? a.Kp >> 6 : 0x7fffffff;  // word steps of one plane
     const int wpiece = lane & 3;
     const uint32_t *wrow[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) wrow[r] = a.wq + (size_t)min(n0 + 16 * r + (lane >> 2), Nc - 1) * KW;
     v4i wr[4];
     auto load_w = [&](int group) __attribute__((always_inline)) {
-        int ws = 4 * group + wpiece;
-        const bool in = ws < wall;
+        const int q = min(GS * group + wpiece / WS, steps - 1);
+        int ws = WS * (q < first ? whole : q - first) + wpiece % WS;
         if constexpr (PLANES) {
             if (ws >= wsteps) ws -= wsteps;
             if (ws >= wsteps) ws -= wsteps;
         }
-        const int have = in ? KW - 4 * ws : 0;
-        if (4 * group + 4 <= (KW >> 2)) {  // (every lane's four words lie in the row: also where planes follow each other, for the first)
+        if ((KW & 3) == 0) {
+            ws = min(ws, (KW >> 2) - 1);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(wrow[r] + 4 * ws);
+            for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(as_global(wrow[r] + 4 * ws));
         } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                Piece<int, 4> v;
-                if (have >= 4) v.load(reinterpret_cast<const int *>(wrow[r] + 4 * ws));
-                else
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v.e[e] = e < have ? (int)wrow[r][4 * ws + e] : 0;
-                wr[r] = v4i{v.e[0], v.e[1], v.e[2], v.e[3]};
-            }
+                for (int e = 0; e < 4; ++e) wr[r][e] = (int)as_global(wrow[r])[min(4 * ws + e, KW - 1)];
         }
     };
     unsigned char *wput = codes + wpiece * kCodeStep + (lane >> 2) * 16;
@@ -176,17 +153,40 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[i][t] = Acc{0, 0, 0, 0};
 
+    int *lrow = reinterpret_cast<int *>(lds + G::ROWS);  // [TM] row, [TM] adapter (kNone: none), [TM] step
+    float *lstep = reinterpret_cast<float *>(lrow + 2 * G::TM);
+    float *lws = reinterpret_cast<float *>(lds + G::CHANS);  // [TN] w_scale, [TN] bias
     load_w(0);
-    load_x(0);
+    for (int i = tid; i < G::TM; i += G::NT) {
+        const int row = a.rows[min(m0 + i, a.m - 1)];
+        const int el = a.hw == 1 ? row : row / a.hw;
+        const int l = a.index[el];
+        lrow[i] = row;
+        lrow[G::TM + i] = m0 + i < a.m && l >= 0 && l < a.adapters ? l : kNone;
+        if constexpr (!PLANES) lstep[i] = a.step[el];
+    }
+    if constexpr (!PLANES) {
+        const int c = min(ntile * G::TN + tid, Nc - 1);
+        lws[tid] = a.w_scale[c];
+        lws[G::TN + tid] = a.bias ? a.bias[c] : 0.0f;
+    }
+    if (first) {
+        const int at = 128 * whole + 16 * piece;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            Piece<int8_t, 16> v;
+            v.load_some(reinterpret_cast<const int8_t *>(as_global(src[q] + at)), row_bytes - at);
+            xr[q] = __builtin_bit_cast(v4i, v);
+        }
+    } else
+        load_x(0);
     put_w();
     load_w(1);
     put_x(0);
-    load_x(1 < steps ? 1 : 0);
-    lora_lds_barrier();
+    if (steps > 1) load_x(1);
+    lds_only_barrier();
 
     const int sw = (j & 7);
-    constexpr int WS = PLANES ? 1 : 2;   // word steps of a step
-    constexpr int GS = 4 / WS;           // steps of a group of codes
     for (int s = 0; s < steps; ++s) {
         const unsigned char *slab = lds + (s & 1) * G::SLAB + j * 128;
         uint32_t wc[WS][4];
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 #pragma unroll
             for (int t = 0; t < 4; ++t) wc[h][t] = *reinterpret_cast<const uint32_t *>(wget + (WS * (s % GS) + h) * kCodeStep + 256 * t);
         put_x((s + 1) & 1);
-        load_x(s + 2 < steps ? s + 2 : steps - 1);
+        if (s + 2 < steps) load_x(s + 2);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v4i B[PT];
@@ -219,18 +219,51 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             put_w();
             load_w(s / GS + 2);
         }
-        lora_lds_barrier();
+        lds_only_barrier();
     }
 
     // ---- epilogue: lane (j, g), register e of tile (i, t): row 16i + j, channel n0 + 16t + 4g + e --------------------
-    int row[PT], group[PT];
+    // Ranks 16 at a time.  All threads bring the tile's hid in, scaled and split into planes, one half of 8 ranks of a row each, into the
+    // slabs that are free by now (two buffers in turn); a wavefront's factors come straight from memory, the first ones on
+    // their way while the sums are scaled.
+    using L = LowPlanes<TO, TA>;
+    const TA *low = as_global(static_cast<const TA *>(a.low));
+    auto low_factors = [&](int l, int r0, TA(&v)[4][8]) __attribute__((always_inline)) {
+        // (a uniform base and 32-bit offsets: rank * channels * 2 bytes are 16 MB at most)
+        const char *from = reinterpret_cast<const char *>(low + (size_t)l * a.rank * Nc);
+        unsigned at[4];
 #pragma unroll
-    for (int i = 0; i < PT; ++i) {
-        const int pos = m0 + 16 * i + j;
-        row[i] = a.rows[min(pos, a.m - 1)];
-        const int el = a.hw == 1 ? row[i] : row[i] / a.hw;
-        group[i] = a.index[el];
-        if (pos >= a.m || group[i] < 0 || group[i] >= a.adapters) group[i] = 0x7fffffff;
+        for (int t = 0; t < 4; ++t) at[t] = (unsigned)min(n0 + 16 * t + j, Nc - 1) * (unsigned)sizeof(TA);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const unsigned r = (unsigned)min(r0 + 8 * (g & 1) + e, a.rank - 1) * (unsigned)Nc * (unsigned)sizeof(TA);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t][e] = *reinterpret_cast<const TA *>(from + r + at[t]);
+        }
+    };
+    int own[PT];  // adapter of row 16i + j
+#pragma unroll
+    for (int i = 0; i < PT; ++i) own[i] = lrow[G::TM + 16 * i + j];
+    auto next_adapter = [&](int after) __attribute__((always_inline)) {  // the wavefront's smallest one above `after`
+        int next = kNone;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) next = own[i] > after ? min(next, own[i]) : next;
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, 64));
+        return __builtin_amdgcn_readfirstlane(next);
+    };
+    const int adapter0 = next_adapter(-1);  // (the same in every wavefront of the workgroup)
+    // this thread's share of hid: half tid & 1 of the 16 ranks of row tid >> 1
+    const int hrow = tid >> 1, hhalf = tid & 1;
+    const bool hmine = hrow < G::TM && lrow[G::TM + min(hrow, G::TM - 1)] != kNone;
+    const float *hfrom = as_global(a.hid) + (size_t)lrow[min(hrow, G::TM - 1)] * a.rank + 8 * hhalf;
+    Piece<float, 8> hv;
+    TA lv[4][8];
+    float hscale = 1.0f;
+    if (adapter0 != kNone) {
+        hv.load_some(hfrom, hmine ? a.rank - 8 * hhalf : 0);
+        if (a.scale && hmine) hscale = a.scale[lrow[G::TM + hrow]];
+        low_factors(adapter0, 0, lv);
     }
     v4f z[PT][4];
     if constexpr (PLANES) {
@@ -239,79 +272,87 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 #pragma unroll
             for (int t = 0; t < 4; ++t) z[i][t] = acc[i][t];
     } else {
-        v4f ws[4], bi[4];
+        float st[PT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int i = 0; i < PT; ++i) st[i] = lstep[16 * i + j];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = min(n0 + 16 * t + 4 * g + e, Nc - 1);
-                ws[t][e] = a.w_scale[c];
-                bi[t][e] = a.bias ? a.bias[c] : 0.0f;
-            }
+        for (int t = 0; t < 4; ++t) {
+            const v4f ws = *reinterpret_cast<const v4f *>(lws + 64 * wave + 16 * t + 4 * g);
+            const v4f bi = *reinterpret_cast<const v4f *>(lws + G::TN + 64 * wave + 16 * t + 4 * g);
 #pragma unroll
-        for (int i = 0; i < PT; ++i) {
-            const float st = a.step[a.hw == 1 ? row[i] : row[i] / a.hw];
+            for (int i = 0; i < PT; ++i)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z[i][t][e] = base_value(acc[i][t][e], ws[t][e], st, bi[t][e]);
+                for (int e = 0; e < 4; ++e) z[i][t][e] = base_value(acc[i][t][e], ws[e], st[i], bi[e]);
         }
     }
-    using L = LowPlanes<TO, TA>;
-    const TA *low = static_cast<const TA *>(a.low);
-    int now = -1;
-    for (;;) {
-        // the wavefront's next adapter: the smallest one above the last
-        int next = 0x7fffffff;
-#pragma unroll
-        for (int i = 0; i < PT; ++i) next = group[i] > now ? min(next, group[i]) : next;
-#pragma unroll
-        for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, 64));
-        now = __builtin_amdgcn_readfirstlane(next);
-        if (now == 0x7fffffff) break;
-        const float f = a.scale ? a.scale[now] : 1.0f;
-        for (int r0 = 0; r0 < a.rank; r0 += 16) {
-            const int rl = r0 + 8 * (g & 1);
-            v8bf A1[4], A2[L::SECOND ? 4 : 1], A3[L::THIRD ? 4 : 1];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int c = min(n0 + 16 * t + j, Nc - 1);
-                TA v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = low[((size_t)now * a.rank + min(rl + e, a.rank - 1)) * Nc + c];
+    if (adapter0 != kNone) {
+        for (int r0 = 0, turn = 0; r0 < a.rank; r0 += 16, turn ^= 1) {
+            unsigned char *planes = lds + turn * G::SLAB;  // [TM][4 slots of 16 bytes], twice
+            if (hrow < G::TM) {
+                v8bf s0, s1, s2;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    bf16_t s[L::LOW];
-                    split<L::LOW>(rl + e < a.rank ? (float)v[e] : 0.0f, s);
-                    A1[t][e] = s[0];
-                    if constexpr (L::THIRD) A3[t][e] = g < 2 ? (bf16_t)0.0f : s[1];
-                    if constexpr (L::SECOND) A2[t][e] = g < 2 ? (L::LOW == 2 ? s[L::LOW - 1] : (bf16_t)0.0f) : s[0];
+                    bf16_t s[3];
+                    split<3>(hv.e[e] * hscale, s);
+                    s0[e] = s[0];
+                    s1[e] = s[1];
+                    s2[e] = s[2];
+                }
+                unsigned char *to = planes + hrow * 64;
+                const int x = (hrow >> 1) & 3;
+                *reinterpret_cast<v8bf *>(to + ((hhalf ^ x) << 4)) = s0;
+                *reinterpret_cast<v8bf *>(to + (((2 + hhalf) ^ x) << 4)) = s1;
+                if constexpr (L::SECOND) {
+                    *reinterpret_cast<v8bf *>(to + G::TM * 64 + ((hhalf ^ x) << 4)) = s0;
+                    *reinterpret_cast<v8bf *>(to + G::TM * 64 + (((2 + hhalf) ^ x) << 4)) = s2;
                 }
             }
+            lds_only_barrier();
+            if (r0 + 16 < a.rank) hv.load_some(hfrom + r0 + 16, hmine ? a.rank - r0 - 16 - 8 * hhalf : 0);
+            const int rl = r0 + 8 * (g & 1);
+            for (int l = adapter0; l != kNone;) {
+                v8bf A1[4], A2[L::SECOND ? 4 : 1], A3[L::THIRD ? 4 : 1];
 #pragma unroll
-            for (int i = 0; i < PT; ++i) {
-                const bool mine = group[i] == now;
-                const unsigned long long here = __ballot(mine);
-                if (here == 0) continue;
-                v8bf b1, b2;
-                hid_operand<L::SECOND>(a.hid + (size_t)row[i] * a.rank + rl, a.rank - rl, f, g, mine, b1, b2);
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    v4f v = mfma_bf16(A1[t], b1, z[i][t]);
-                    if constexpr (L::SECOND) v = mfma_bf16(A2[t], b2, v);
-                    if constexpr (L::THIRD) v = mfma_bf16(A3[t], b1, v);
-                    if (here == ~0ull) z[i][t] = v;
-                    else  // (zeros in the others' place would not keep an infinity of this adapter from their rows)
+                    for (int e = 0; e < 8; ++e) {
+                        bf16_t s[L::LOW];
+                        split<L::LOW>(rl + e < a.rank ? (float)lv[t][e] : 0.0f, s);
+                        A1[t][e] = s[0];
+                        if constexpr (L::SECOND) A2[t][e] = g < 2 ? (L::LOW == 2 ? s[L::LOW - 1] : (bf16_t)0.0f) : s[0];
+                        if constexpr (L::THIRD) A3[t][e] = g < 2 ? (bf16_t)0.0f : s[L::LOW - 1];
+                    }
+                const int after = next_adapter(l);
+                if (after != kNone) low_factors(after, r0, lv);
+                else if (r0 + 16 < a.rank) low_factors(adapter0, r0 + 16, lv);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) z[i][t][e] = mine ? v[e] : z[i][t][e];
+                for (int i = 0; i < PT; ++i) {
+                    const bool mine = own[i] == l;
+                    const unsigned long long here = __ballot(mine);
+                    if (here == 0) continue;
+                    const unsigned char *from = planes + (16 * i + j) * 64 + ((g ^ ((j >> 1) & 3)) << 4);
+                    const v8bf b1 = *reinterpret_cast<const v8bf *>(from);
+                    v8bf b2;
+                    if constexpr (L::SECOND) b2 = *reinterpret_cast<const v8bf *>(from + G::TM * 64);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        v4f v = mfma_bf16(A1[t], b1, z[i][t]);
+                        if constexpr (L::SECOND) v = mfma_bf16(A2[t], b2, v);
+                        if constexpr (L::THIRD) v = mfma_bf16(A3[t], b1, v);
+                        if (here == ~0ull) z[i][t] = v;
+                        else  // (what another adapter makes of this row's hid is dropped, whatever it is)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[i][t][e] = mine ? v[e] : z[i][t][e];
+                    }
                 }
+                l = after;
             }
         }
     }
     // out through the wavefront's own LDS: 16 rows x 64 channels at a time, rows in whole runs
     constexpr int PITCH = 64 * (int)sizeof(TO) + 16;
     constexpr int VE = 16 / sizeof(TO), PR = 64 / VE;  // elements of a piece, pieces of a row
-    TO *y = static_cast<TO *>(a.y);
+    TO *y = as_global(static_cast<TO *>(a.y));
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
 #pragma unroll
@@ -327,8 +368,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             const int rr = idx / PR, c = idx % PR * VE;
             Piece<TO, VE> o;
             o.load(reinterpret_cast<const TO *>(codes + rr * PITCH) + c);
-            const int dst = __shfl(row[i], rr, 64);
-            if (m0 + 16 * i + rr < a.m) o.store_some(y + (size_t)dst * Nc + n0 + c, Nc - n0 - c);
+            if (m0 + 16 * i + rr < a.m) o.store_some(y + (size_t)lrow[16 * i + rr] * Nc + n0 + c, Nc - n0 - c);
         }
     }
 }

@@ -161,9 +161,10 @@ __global__ __launch_bounds__(norm_threads(WPR)) void norm_kernel(const NormArgs 
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------
-// A workgroup takes every gridDim.x-th group of rows and keeps its sums for dweight and dbias in registers from row
+// A workgroup of 16 wavefronts takes every gridDim.x-th group of rows and keeps its sums for dweight and dbias in registers from row
 // to row (each lane owns its columns in all of them); they meet in LDS once at the end and leave as one row of
 // partial sums per workgroup.  A second kernel adds the rows up in their order: no atomics, the same bits every time.
+// The next row is on its way while one is worked on (up to two pieces a lane; more of them fill the registers).
 struct NormGradArgs {
     const void *dy, *x;
     const float *weight, *mean, *rstd;
@@ -173,18 +174,21 @@ struct NormGradArgs {
     int cols, want;  // want: whether dweight or dbias is asked for
 };
 
+constexpr int kNormGradWaves = 16;
+
 template <typename T, int NV, int WPR>
-__global__ __launch_bounds__(norm_threads(WPR)) void norm_grad_kernel(const NormGradArgs a)
+__global__ __launch_bounds__(64 * kNormGradWaves) void norm_grad_kernel(const NormGradArgs a)
 {
-    using G = NormGeom<T, NV, WPR>;
-    constexpr int VE = G::VE;
-    __shared__ float part[2][2][G::WAVES];
+    constexpr int VE = 16 / sizeof(T);
+    constexpr int ROWS = kNormGradWaves / WPR;
+    __shared__ float part[2][2][kNormGradWaves];
     extern __shared__ float sums[];  // [2][cols] when ROWS > 1
     const int lane = threadIdx.x & 63;
-    const int wave = threadIdx.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wv = wave % WPR, slot = wave / WPR;
     const int C = a.cols;
     const float inv = 1.0f / (float)C;
+    const bool full = C == 64 * VE * NV * WPR;  // every lane has all of its columns
 
     float dw[NV][VE], db[NV][VE];
 #pragma unroll
@@ -192,51 +196,74 @@ __global__ __launch_bounds__(norm_threads(WPR)) void norm_grad_kernel(const Norm
 #pragma unroll
         for (int e = 0; e < VE; ++e) dw[i][e] = db[i][e] = 0.0f;
 
-    int turn = 0;
-    for (long long r0 = (long long)blockIdx.x * G::ROWS; r0 < a.rows; r0 += (long long)gridDim.x * G::ROWS) {
-        const bool live = r0 + slot < a.rows;
-        const long long row = live ? r0 + slot : a.rows - 1;
-        const T *x = static_cast<const T *>(a.x) + row * C;
-        const T *dy = static_cast<const T *>(a.dy) + row * C;
-        Piece<T, VE> xv[NV], gv[NV];
+    auto all_rows = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        auto load = [&](long long r, Piece<T, VE>(&xv)[NV], Piece<T, VE>(&gv)[NV], float &m, float &rs) __attribute__((always_inline)) {
+            const T *x = static_cast<const T *>(a.x) + r * C;
+            const T *dy = static_cast<const T *>(a.dy) + r * C;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
-            xv[i].load_some(x + c0, C - c0);
-            gv[i].load_some(dy + c0, C - c0);
-        }
-        const float m = a.mean[row], rs = a.rstd[row];
-        float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
-            Piece<float, VE> w;
-            load_vector<VE>(w, a.weight, c0, C - c0, 1.0f);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float d = (float)gv[i].e[e];
-                const float h = ((float)xv[i].e[e] - m) * rs;
-                const bool in = e < C - c0;
-                if (in && live) {
-                    dw[i][e] += d * h;
-                    db[i][e] += d;
-                }
-                const float g = d * w.e[e];
-                s1 += in ? g : 0.0f;
-                s2 += in ? g * h : 0.0f;
+            for (int i = 0; i < NV; ++i) {
+                const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
+                xv[i].load_some(x + c0, WHOLE ? VE : C - c0);
+                gv[i].load_some(dy + c0, WHOLE ? VE : C - c0);
             }
-        }
-        if (a.dx) {
+            m = a.mean[r];
+            rs = a.rstd[r];
+        };
+        const long long by = (long long)gridDim.x * ROWS;
+        long long r0 = (long long)blockIdx.x * ROWS;
+        constexpr bool AHEAD = NV <= 2;
+        Piece<T, VE> xn[NV], gn[NV];
+        float mn, rn;
+        if constexpr (AHEAD) load(min(r0 + slot, a.rows - 1), xn, gn, mn, rn);
+        int turn = 0;
+        for (; r0 < a.rows; r0 += by) {
+            const bool live = r0 + slot < a.rows;
+            const long long row = live ? r0 + slot : a.rows - 1;
+            Piece<T, VE> xv[NV], gv[NV];
+            float m, rs;
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    xv[i] = xn[i];
+                    gv[i] = gn[i];
+                }
+                m = mn;
+                rs = rn;
+                if (r0 + by < a.rows) load(min(r0 + by + slot, a.rows - 1), xn, gn, mn, rn);
+            } else
+                load(row, xv, gv, m, rs);
+            float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
+                Piece<float, VE> w;
+                load_vector<VE>(w, a.weight, c0, WHOLE ? VE : C - c0, 1.0f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const float d = (float)gv[i].e[e];
+                    const float h = ((float)xv[i].e[e] - m) * rs;
+                    const bool in = WHOLE || e < C - c0;
+                    if (in && live) {
+                        dw[i][e] += d * h;
+                        db[i][e] += d;
+                    }
+                    const float g = d * w.e[e];
+                    s1 += in ? g : 0.0f;
+                    s2 += in ? g * h : 0.0f;
+                }
+            }
+            if (!a.dx) continue;
             s1 = wave_sum_f32(s1);
             s2 = wave_sum_f32(s2);
             if constexpr (WPR > 1) {
-                // (two sets of slots in turn: one barrier per row)
+                // (two sets of slots in turn: one barrier per row, and one that leaves the next row's loads on their way)
                 float *p1 = &part[turn & 1][0][slot * WPR], *p2 = &part[turn & 1][1][slot * WPR];
                 if (lane == 0) {
                     p1[wv] = s1;
                     p2[wv] = s2;
                 }
-                __syncthreads();
+                lds_only_barrier();
                 s1 = p1[0];
                 s2 = p2[0];
 #pragma unroll
@@ -251,76 +278,83 @@ __global__ __launch_bounds__(norm_threads(WPR)) void norm_grad_kernel(const Norm
             for (int i = 0; i < NV; ++i) {
                 const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
                 Piece<float, VE> w;
-                load_vector<VE>(w, a.weight, c0, C - c0, 1.0f);
+                load_vector<VE>(w, a.weight, c0, WHOLE ? VE : C - c0, 1.0f);
                 Piece<T, VE> o;
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
                     const float h = ((float)xv[i].e[e] - m) * rs;
                     o.e[e] = (T)(((float)gv[i].e[e] * w.e[e] - c1 - h * c2) * rs);
                 }
-                if (live) o.store_some(static_cast<T *>(a.dx) + row * C + c0, C - c0);
+                if (live) o.store_some(static_cast<T *>(a.dx) + row * C + c0, WHOLE ? VE : C - c0);
             }
         }
-    }
+    };
+    if (full) all_rows(std::true_type{});
+    else all_rows(std::false_type{});
+
     if (!a.want) return;
     float *out = a.part + (size_t)blockIdx.x * 2 * C;
-    if constexpr (G::ROWS == 1) {
+    // the groups of wavefronts one after the other through LDS, the last one to memory
+    for (int k = 0; k < ROWS; ++k) {
+        if (k) __syncthreads();
+        if (slot == k) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
-            Piece<float, VE> p;
+            for (int i = 0; i < NV; ++i) {
+                const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
+                Piece<float, VE> w, b;
+                if (k) {
+                    w.load_some(sums + c0, C - c0);
+                    b.load_some(sums + C + c0, C - c0);
+                }
 #pragma unroll
-            for (int e = 0; e < VE; ++e) p.e[e] = dw[i][e];
-            p.store_some(out + c0, C - c0);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) p.e[e] = db[i][e];
-            p.store_some(out + C + c0, C - c0);
-        }
-    } else {
-        // the rows of the workgroup one after the other through LDS
-        for (int k = 0; k < G::ROWS; ++k) {
-            __syncthreads();
-            if (slot == k) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e)
-                        if (e < C - c0) {
-                            const float w = k ? sums[c0 + e] + dw[i][e] : dw[i][e];
-                            const float b = k ? sums[C + c0 + e] + db[i][e] : db[i][e];
-                            if (k < G::ROWS - 1) {
-                                sums[c0 + e] = w;
-                                sums[C + c0 + e] = b;
-                            } else {
-                                out[c0 + e] = w;
-                                out[C + c0 + e] = b;
-                            }
-                        }
+                for (int e = 0; e < VE; ++e) {
+                    w.e[e] = k ? w.e[e] + dw[i][e] : dw[i][e];
+                    b.e[e] = k ? b.e[e] + db[i][e] : db[i][e];
+                }
+                if (k < ROWS - 1) {
+                    w.store_some(sums + c0, C - c0);
+                    b.store_some(sums + C + c0, C - c0);
+                } else {
+                    w.store_some(out + c0, C - c0);
+                    b.store_some(out + C + c0, C - c0);
                 }
             }
         }
     }
 }
 
-// Column sums of the partial rows: 64 columns per workgroup, 4 wavefronts a quarter of the rows each.
+// Column sums of the partial rows: 64 columns per workgroup, 4 per lane, 16 slices of the rows, then the slices.
 __global__ __launch_bounds__(256) void norm_grad_sum_kernel(const float *__restrict__ part, int parts, int cols,
                                                             float *__restrict__ dweight, float *__restrict__ dbias)
 {
-    __shared__ float s[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
-    float v = 0.0f;
-    if (c < 2 * cols)
-        for (int p = wave; p < parts; p += 4) v += part[(size_t)p * 2 * cols + c];
-    s[wave][lane] = v;
+    __shared__ v4f s[16][16];
+    const int q = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const int c = blockIdx.x * 64 + 4 * q;
+    v4f v = {0, 0, 0, 0};
+    if (c + 4 <= 2 * cols) {
+#pragma unroll 8
+        for (int p = slice; p < parts; p += 16) {
+            Piece<float, 4> x;
+            x.load(part + (size_t)p * 2 * cols + c);
+            v += v4f{x.e[0], x.e[1], x.e[2], x.e[3]};
+        }
+    } else if (c < 2 * cols) {
+        for (int p = slice; p < parts; p += 16)
+            for (int e = 0; e < 4; ++e)
+                if (c + e < 2 * cols) v[e] += part[(size_t)p * 2 * cols + c + e];
+    }
+    s[slice][q] = v;
     __syncthreads();
-    if (wave == 0 && c < 2 * cols) {
-        v = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
-        if (c < cols) {
-            if (dweight) dweight[c] = v;
-        } else if (dbias)
-            dbias[c - cols] = v;
+    if (slice == 0) {
+#pragma unroll
+        for (int k = 1; k < 16; ++k) v += s[k][q];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e < cols) {
+                if (dweight) dweight[c + e] = v[e];
+            } else if (c + e < 2 * cols && dbias)
+                dbias[c + e - cols] = v[e];
+        }
     }
 }
 
@@ -353,9 +387,8 @@ template <typename T, int NV, int WPR> static void norm_launch(const NormArgs &a
 }
 template <typename T, int NV, int WPR> static void norm_grad_launch(const NormGradArgs &a, int parts, hipStream_t st)
 {
-    using G = NormGeom<T, NV, WPR>;
-    hipLaunchKernelGGL((norm_grad_kernel<T, NV, WPR>), dim3((unsigned)parts), dim3(64 * G::WAVES),
-                       G::ROWS > 1 && a.want ? (size_t)8 * a.cols : 0, st, a);
+    hipLaunchKernelGGL((norm_grad_kernel<T, NV, WPR>), dim3((unsigned)parts), dim3(64 * kNormGradWaves),
+                       WPR < kNormGradWaves && a.want ? (size_t)8 * a.cols : 0, st, a);
 }
 // f(NV, WPR) as integral constants
 template <typename F> static void norm_pick(int nv, int wpr, F f)
@@ -406,10 +439,15 @@ static int norm_forward(const void *x, int type, long long rows, int cols, const
     return check_launch();
 }
 
+// Wavefronts per row of the gradient kernel: as few as hold the row in two pieces a lane, and 16 beyond that.
+static int norm_grad_wpr(int cols, int bytes)
+{
+    const int held = 64 * 2 * (16 / bytes);
+    return cols <= held ? 1 : cols <= 4 * held ? 4 : 16;
+}
 static int norm_grad_parts(long long rows, int cols, int bytes)
 {
-    const int wpr = norm_wpr(rows, cols, bytes);
-    const int per = wpr < kNormWaves ? kNormWaves / wpr : 1;
+    const int per = kNormGradWaves / norm_grad_wpr(cols, bytes);
     const long long groups = (rows + per - 1) / per;
     return (int)(groups < kNormParts ? groups : kNormParts);
 }
@@ -454,7 +492,7 @@ extern "C" int prom_layernorm_backward(const void *dy, const void *x, int type, 
     if (outputs_meet(out, 4, in, 5)) return PROM_EALIAS;
     const int parts = norm_grad_parts(rows, cols, bytes);
     const NormGradArgs a{dy, x, weight, mean, rstd, dx, static_cast<float *>(workspace), rows, cols, want ? 1 : 0};
-    const int wpr = norm_wpr(rows, cols, bytes), nv = norm_nv(cols, wpr, bytes);
+    const int wpr = norm_grad_wpr(cols, bytes), nv = norm_nv(cols, wpr, bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
     clear_hip_error();
     norm_type(type, [&](auto t) {

@@ -108,7 +108,7 @@ template <bool BACK, typename TX, typename TA, int RT>
 __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a)
 {
     constexpr int PA = planes_of<TA>();
-    constexpr int PX = BACK ? planes_of<TX>() : 1;
+    constexpr int PX = BACK ? planes_of<TX>() : 1;  // (codes: one plane)
     constexpr int KS = BACK ? 32 : 64;  // channels of a step
     constexpr int KL = KS / 4;          // of them a lane's
     __shared__ v4f red[4][2 * RT][64];
@@ -139,56 +139,70 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
         for (int t = 0; t < RT; ++t) acc[i][t] = v4f{0, 0, 0, 0};
 
     const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * K;
-    const int limit = BACK && a.planes ? a.Kp : K;
-    for (int k = KS * wave; k < limit && (BACK || has); k += KS * 8) {
-        const int k0 = k + KL * g;
-        v8bf bx[2][BACK ? PX : 2];
-        if constexpr (BACK) {
-            Piece<TX, 8> v[2];
+    // U steps of loads leave together before the first of them is used: with 32 rows to a workgroup there are no more than
+    // 2 wavefronts on a SIMD to wait with (rank 32, 8192 x 4096: 20 us with one step at a time)
+    constexpr int U = RT <= 2 ? 4 : RT == 4 ? 2 : 1;
+    auto steps = [&](auto whole, int k, int by, int u) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int N = WHOLE ? U : 1;
+        Piece<TX, BACK ? 8 : 16> v[N][2];
+        Piece<float, 8> ws[N];
+        Piece<TA, 8> w[N][RT][KL / 8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v[i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, K - k0);
-            if (a.planes) {
-                Piece<float, 8> ws;
-                ws.load_some(a.w_scale + k0, K - k0);
+        for (int n = 0; n < N; ++n) {
+            const int k0 = k + (n < u ? n : 0) * by + KL * g;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
+            if (BACK && a.planes) ws[n].load_some(a.w_scale + k0, WHOLE ? 8 : K - k0);
+            if (has)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const int r = min(16 * t + j, a.rank - 1);  // (ranks past the last one repeat it and are not written)
+#pragma unroll
+                    for (int h = 0; h < KL / 8; ++h) w[n][t][h].load_some(low + (size_t)r * K + k0 + 8 * h, WHOLE ? 8 : K - k0 - 8 * h);
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (n >= u) break;
+            const int k0 = k + n * by + KL * g;
+            v8bf bx[2][BACK ? PX : 2];
+            if constexpr (BACK) {
+                if (a.planes) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        Piece<bf16_t, 8> o[PX];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            bf16_t s[PX];
+                            split<PX>((float)v[n][i].e[e] * ws[n].e[e] * 0.5f, s);
+                            // (the decoded codes come in the order 0, 2, 1, 3 of every four)
+                            constexpr int to[8] = {0, 2, 1, 3, 4, 6, 5, 7};
+#pragma unroll
+                            for (int p = 0; p < PX; ++p) o[p].e[to[e]] = s[p];
+                        }
+                        const size_t pos = (size_t)(tile.y + 16 * i + j);
+                        if (in[i])
+#pragma unroll
+                            for (int p = 0; p < PX; ++p) o[p].store(a.planes + (pos * PX + p) * a.Kp + k0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) split_piece<PX>(v[n][i], bx[i]);
+            } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    Piece<bf16_t, 8> o[PX];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        bf16_t s[PX];
-                        split<PX>((float)v[i].e[e] * ws.e[e] * 0.5f, s);
-                        // (the decoded codes come in the order 0, 2, 1, 3 of every four)
-                        constexpr int to[8] = {0, 2, 1, 3, 4, 6, 5, 7};
-#pragma unroll
-                        for (int p = 0; p < PX; ++p) o[p].e[to[e]] = s[p];
-                    }
-                    const size_t pos = (size_t)(tile.y + 16 * i + j);
-                    if (in[i])
-#pragma unroll
-                        for (int p = 0; p < PX; ++p) o[p].store(a.planes + (pos * PX + p) * a.Kp + k0);
+                    bx[i][0] = codes_to_bf16(v[n][i].e);
+                    bx[i][1] = codes_to_bf16(v[n][i].e + 8);
                 }
             }
+            if (!has) continue;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) split_piece<PX>(v[i], bx[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                Piece<int8_t, 16> v;
-                v.load_some(static_cast<const int8_t *>(a.in) + (size_t)row[i] * K + k0, K - k0);
-                bx[i][0] = codes_to_bf16(v.e);
-                bx[i][1] = codes_to_bf16(v.e + 8);
-            }
-        }
-        if (has) {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                const int r = min(16 * t + j, a.rank - 1);  // (ranks past the last one repeat it and are not written)
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int h = 0; h < KL / 8; ++h) {
-                    Piece<TA, 8> w;
-                    w.load_some(low + (size_t)r * K + k0 + 8 * h, K - k0 - 8 * h);
                     v8bf aw[PA];
-                    split_piece<PA>(w, aw);
+                    split_piece<PA>(w[n][t][h], aw);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if constexpr (BACK) {
@@ -203,8 +217,17 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                         }
                     }
                 }
-            }
         }
+    };
+    if (BACK || has) {
+        constexpr int BY = KS * 8;  // from one step of a wavefront to its next
+        const int end = K / KS * KS;
+        int k = KS * wave;
+        for (; k < end; k += U * BY) steps(std::true_type{}, k, BY, min(U, (end - k + BY - 1) / BY));
+        // what is left behind the whole steps, and the planes' padding
+        const int limit = BACK && a.planes ? a.Kp : K;
+        for (k = end; k < limit; k += KS)
+            if ((k / KS & 7) == wave) steps(std::false_type{}, k, 0, 1);
     }
     // sums of the 8 wavefronts, always added in the same order
     if (wave >= 4)
@@ -318,48 +341,77 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[t][e] = v4f{0, 0, 0, 0};
 
-    for (int m = 0; m < chunk.z; m += 32) {
-        const int have = chunk.z - m - 8 * g;  // rows of this lane
-        Piece<int, 8> row;
-        row.load_some(a.rows + chunk.y + m + 8 * g, have);
-        Piece<TX, 8> v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e].load_some(static_cast<const TX *>(a.in) + (size_t)row.e[e] * a.C + c0, e < have ? a.C - c0 : 0);
-        v8bf co[RT][3];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int r = min(r0 + 16 * t + j, a.rank - 1);
+    // Row numbers are fetched two steps of 32 rows ahead, rows and coefficients one.  (The next step's loads behind the
+    // last one repeat it: they are not used.)
+    auto all_rows = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;  // every step has 32 rows and every lane 8 columns
+        auto load_rows = [&](int m, Piece<int, 8> &row) __attribute__((always_inline)) {
+            row.load_some(a.rows + chunk.y + m + 8 * g, WHOLE ? 8 : chunk.z - m - 8 * g);
+        };
+        auto load = [&](int m, const Piece<int, 8> &row, Piece<TX, 8>(&v)[8], float(&c)[RT][8]) __attribute__((always_inline)) {
+            const int have = WHOLE ? 8 : chunk.z - m - 8 * g;  // rows of this lane
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float c = e < have ? a.coef[(size_t)row.e[e] * a.rank + r] * f : 0.0f;
-                bf16_t s[3];
-                split<3>(c, s);
+                v[e].load_some(static_cast<const TX *>(a.in) + (size_t)row.e[e] * a.C + c0, WHOLE ? 8 : e < have ? a.C - c0 : 0);
 #pragma unroll
-                for (int p = 0; p < 3; ++p) co[t][p][e] = s[p];
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            v8bf b[PX];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (CODES) b[0][e] = (bf16_t)(float)v[e].e[c];
-                else {
-                    bf16_t s[PX];
-                    split<PX>((float)v[e].e[c], s);
-#pragma unroll
-                    for (int p = 0; p < PX; ++p) b[p][e] = s[p];
+                for (int t = 0; t < RT; ++t) {
+                    c[t][e] = 0.0f;
+                    if (e < have) c[t][e] = a.coef[(size_t)row.e[e] * a.rank + min(r0 + 16 * t + j, a.rank - 1)];
                 }
             }
+        };
+        Piece<int, 8> row;
+        Piece<TX, 8> v[8];
+        float cf[RT][8];
+        load_rows(0, row);
+        load(0, row, v, cf);
+        const int last = (chunk.z - 1) & ~31;
+        load_rows(min(32, last), row);
+        for (int m = 0; m < chunk.z; m += 32) {
+            Piece<TX, 8> now[8];
+            v8bf co[RT][3];
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
+            for (int e = 0; e < 8; ++e) {
+                now[e] = v[e];
 #pragma unroll
-                for (int p = 0; p < 3; ++p)
+                for (int t = 0; t < RT; ++t) {
+                    bf16_t s[3];
+                    split<3>(cf[t][e] * f, s);
 #pragma unroll
-                    for (int q = 0; q < PX; ++q)
-                        if (p + q < 3) acc[t][c] = mfma_bf16(co[t][p], b[q], acc[t][c]);
+                    for (int p = 0; p < 3; ++p) co[t][p][e] = s[p];
+                }
+            }
+            if (m < last) {
+                load(m + 32, row, v, cf);
+                load_rows(min(m + 64, last), row);
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                v8bf b[PX];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (CODES) b[0][e] = (bf16_t)(float)now[e].e[c];
+                    else if constexpr (PX == 1) b[0][e] = now[e].e[c];
+                    else {
+                        bf16_t s[PX];
+                        split<PX>((float)now[e].e[c], s);
+#pragma unroll
+                        for (int p = 0; p < PX; ++p) b[p][e] = s[p];
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p)
+#pragma unroll
+                        for (int q = 0; q < PX; ++q)
+                            if (p + q < 3) acc[t][c] = mfma_bf16(co[t][p], b[q], acc[t][c]);
+            }
         }
-    }
+    };
+    const int col = (int)(blockIdx.y * 4 + wave) * 128;
+    if ((chunk.z & 31) == 0 && col + 128 <= a.C) all_rows(std::true_type{});
+    else all_rows(std::false_type{});
     // lane (j, g), register e of tile (t, c): rank 16t + 4g + e, column c0 + c
     float *out = a.part + (size_t)blockIdx.x * a.rank * a.C;
 #pragma unroll
@@ -559,7 +611,7 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     sa.adapters = lora->adapters;
     by_adapter_type(lora->type, [&](auto t) {
         by_rank(lora->rank, [&](auto rt) {
-            hipLaunchKernelGGL((lora_shrink_kernel<false, float, decltype(t), decltype(rt)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
+            hipLaunchKernelGGL((lora_shrink_kernel<false, int8_t, decltype(t), decltype(rt)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
         });
     });
     ga.rows = p.rows;

@@ -59,6 +59,8 @@ template <int PT, int NW> struct LoraGeom {
     static constexpr int SLAB = TM * 128;
     static constexpr int OUT = 16 * (64 * 4 + 16);  // a wavefront's 16 rows x 64 channels on their way out (float32 at most)
     static constexpr int WAVE = kCodeBytes > OUT ? kCodeBytes : OUT;
+    static constexpr int LOWS = 16 * (TN * 2 + 16);  // factors of 16 ranks
+    static_assert(2 * LOWS <= NW * WAVE, "two buffers of them fit the wavefronts' own places");
     static constexpr int ROWS = 2 * SLAB + NW * WAVE;       // row, adapter, step of every row
     static constexpr int CHANS = ROWS + TM * 12;            // w_scale, bias of every channel
     static constexpr size_t LDS = (size_t)CHANS + TN * 8;
@@ -223,22 +225,27 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     }
 
     // ---- epilogue: lane (j, g), register e of tile (i, t): row 16i + j, channel n0 + 16t + 4g + e --------------------
-    // Ranks 16 at a time.  All threads bring the tile's hid in, scaled and split into planes, one half of 8 ranks of a row each, into the
-    // slabs that are free by now (two buffers in turn); a wavefront's factors come straight from memory, the first ones on
-    // their way while the sums are scaled.
+    // Ranks 16 at a time, adapter after adapter (the same ones in every wavefront: all own the same rows).  All threads bring the tile's hid
+    // in, scaled and split into planes, one half of 8 ranks of a row each, into the slabs that are free by now, and an adapter's
+    // factors [16 ranks][TN channels] into the codes' place; both have two buffers in turn, and the next ones are on their way in
+    // registers while the last ones are used.
     using L = LowPlanes<TO, TA>;
+    constexpr int LP = G::TN * 2 + 16;  // bytes between ranks
     const TA *low = as_global(static_cast<const TA *>(a.low));
-    auto low_factors = [&](int l, int r0, TA(&v)[4][8]) __attribute__((always_inline)) {
-        // (a uniform base and 32-bit offsets: rank * channels * 2 bytes are 16 MB at most)
-        const char *from = reinterpret_cast<const char *>(low + (size_t)l * a.rank * Nc);
-        unsigned at[4];
+    Piece<TA, 8> lv[2];
+    auto load_low = [&](int l, int r0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) at[t] = (unsigned)min(n0 + 16 * t + j, Nc - 1) * (unsigned)sizeof(TA);
+        for (int q = 0; q < 2; ++q) {
+            const int idx = tid + G::NT * q;
+            const int r = idx / (G::TN / 8), c = ntile * G::TN + idx % (G::TN / 8) * 8;
+            lv[q].load_some(low + ((size_t)l * a.rank + min(r0 + r, a.rank - 1)) * Nc + c, r0 + r < a.rank ? Nc - c : 0);
+        }
+    };
+    auto put_low = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned r = (unsigned)min(r0 + 8 * (g & 1) + e, a.rank - 1) * (unsigned)Nc * (unsigned)sizeof(TA);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) v[t][e] = *reinterpret_cast<const TA *>(from + r + at[t]);
+        for (int q = 0; q < 2; ++q) {
+            const int idx = tid + G::NT * q;
+            lv[q].store(reinterpret_cast<TA *>(lds + 2 * G::SLAB + buffer * G::LOWS + idx / (G::TN / 8) * LP) + idx % (G::TN / 8) * 8);
         }
     };
     int own[PT];  // adapter of row 16i + j
@@ -258,12 +265,11 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     const bool hmine = hrow < G::TM && lrow[G::TM + min(hrow, G::TM - 1)] != kNone;
     const float *hfrom = as_global(a.hid) + (size_t)lrow[min(hrow, G::TM - 1)] * a.rank + 8 * hhalf;
     Piece<float, 8> hv;
-    TA lv[4][8];
     float hscale = 1.0f;
     if (adapter0 != kNone) {
         hv.load_some(hfrom, hmine ? a.rank - 8 * hhalf : 0);
         if (a.scale && hmine) hscale = a.scale[lrow[G::TM + hrow]];
-        low_factors(adapter0, 0, lv);
+        load_low(adapter0, 0);
     }
     v4f z[PT][4];
     if constexpr (PLANES) {
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         }
     }
     if (adapter0 != kNone) {
-        for (int r0 = 0, turn = 0; r0 < a.rank; r0 += 16, turn ^= 1) {
+        for (int r0 = 0, turn = 0, buffer = 0; r0 < a.rank; r0 += 16, turn ^= 1) {
             unsigned char *planes = lds + turn * G::SLAB;  // [TM][4 slots of 16 bytes], twice
             if (hrow < G::TM) {
                 v8bf s0, s1, s2;
@@ -307,24 +313,29 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
                     *reinterpret_cast<v8bf *>(to + G::TM * 64 + (((2 + hhalf) ^ x) << 4)) = s2;
                 }
             }
-            lds_only_barrier();
-            if (r0 + 16 < a.rank) hv.load_some(hfrom + r0 + 16, hmine ? a.rank - r0 - 16 - 8 * hhalf : 0);
-            const int rl = r0 + 8 * (g & 1);
             for (int l = adapter0; l != kNone;) {
+                put_low(buffer);
+                lds_only_barrier();
+                const int after = next_adapter(l);
+                if (after != kNone) load_low(after, r0);
+                else if (r0 + 16 < a.rank) {
+                    load_low(adapter0, r0 + 16);
+                    hv.load_some(hfrom + r0 + 16, hmine ? a.rank - r0 - 16 - 8 * hhalf : 0);
+                }
                 v8bf A1[4], A2[L::SECOND ? 4 : 1], A3[L::THIRD ? 4 : 1];
+                const TA *factors = reinterpret_cast<const TA *>(lds + 2 * G::SLAB + buffer * G::LOWS + 8 * (g & 1) * LP) + 64 * wave + j;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         bf16_t s[L::LOW];
-                        split<L::LOW>(rl + e < a.rank ? (float)lv[t][e] : 0.0f, s);
+                        const TA v = factors[e * (LP / 2) + 16 * t];
+                        if constexpr (std::is_same<TA, bf16_t>::value) s[0] = v;
+                        else split<L::LOW>((float)v, s);
                         A1[t][e] = s[0];
                         if constexpr (L::SECOND) A2[t][e] = g < 2 ? (L::LOW == 2 ? s[L::LOW - 1] : (bf16_t)0.0f) : s[0];
                         if constexpr (L::THIRD) A3[t][e] = g < 2 ? (bf16_t)0.0f : s[L::LOW - 1];
                     }
-                const int after = next_adapter(l);
-                if (after != kNone) low_factors(after, r0, lv);
-                else if (r0 + 16 < a.rank) low_factors(adapter0, r0 + 16, lv);
 #pragma unroll
                 for (int i = 0; i < PT; ++i) {
                     const bool mine = own[i] == l;
@@ -346,8 +357,10 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
                     }
                 }
                 l = after;
+                buffer ^= 1;
             }
         }
+        lds_only_barrier();
     }
     // out through the wavefront's own LDS: 16 rows x 64 channels at a time, rows in whole runs
     constexpr int PITCH = 64 * (int)sizeof(TO) + 16;

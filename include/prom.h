@@ -509,15 +509,16 @@ typedef struct {
  *   w_packed  dev, prom_pack_ternary output for [cout][cin];  w_scale dev float32 [cout];  bias dev float32 [cout] or NULL
  *   y         dev [n][h][w][cout] of y_type: PROM_F32 or the adapters' type
  *   hid       dev float32 [n*h*w][rank] or NULL: what prom_pw_conv_lora_backward takes
- *   workspace dev, 256-byte aligned, at least prom_pw_conv_lora_workspace_size(...) bytes (0 for sizes that are refused); contents
- *             undefined afterwards.  Two calls that can overlap in time need one each.
+ *   workspace dev, 256-byte aligned, at least prom_pw_conv_lora_workspace_size(...) bytes; contents undefined afterwards.  Two calls that
+ *             can overlap in time need one each.  has_hid: whether hid is given; up to 64 rows need no workspace then (0 bytes, as for
+ *             sizes that the call refuses).
  * Any channels, rows, rank and alignment to elements (w_packed: 4 bytes).  PROM_EINVAL for null or misaligned pointers,
  * non-positive sizes, other types; PROM_EUNSUPPORTED above 65536 channels, rank 128, 65535 adapters or 2^30 - 1 rows; PROM_EALIAS if an
  * output overlaps an input or another output; PROM_EWORKSPACE. */
 int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, const void *w_packed, int cout, const float *x_step,
                       const float *w_scale, const float *bias, const prom_lora_t *lora, void *y, int y_type, float *hid,
                       void *workspace, size_t workspace_bytes, void *stream);
-size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank);
+size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank, int has_hid);
 
 /* Its gradients, with the shared weights frozen and the activations' rounding passed straight through: with
  * g[m][r] = scale[l] * sum_co dy[m][co] * b[l][r][co],

@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -195,7 +196,7 @@ def load_library():
     lib.prom_pw_conv_lora.restype = ci
     lib.prom_pw_conv_lora.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp, vp, vp, ctypes.POINTER(_LoraC), vp, ci, vp, vp, sz, vp]
     lib.prom_pw_conv_lora_workspace_size.restype = sz
-    lib.prom_pw_conv_lora_workspace_size.argtypes = [ci] * 7
+    lib.prom_pw_conv_lora_workspace_size.argtypes = [ci] * 8
     lib.prom_pw_conv_lora_backward.restype = ci
     lib.prom_pw_conv_lora_backward.argtypes = [vp, ci, vp, ci, ci, ci, ci, vp, ci, vp, vp, ctypes.POINTER(_LoraC), vp, vp, vp, vp, vp, sz, vp]
     lib.prom_pw_conv_lora_backward_workspace_size.restype = sz
@@ -619,49 +620,57 @@ def _type_of(dtype) -> int:
     if _types is None:
         torch = _torch or _import_torch()
         _types = {torch.float32: PROM_F32, torch.bfloat16: PROM_BF16, torch.float16: PROM_F16}
-    try:
-        return _types[dtype]
-    except KeyError:
-        raise TypeError(f"{dtype} is not float32, bfloat16 or float16") from None
+    t = _types.get(dtype)
+    if t is None:
+        raise TypeError(f"{dtype} is not float32, bfloat16 or float16")
+    return t
 
 
-def _dev(t, name, dtype=None, shape=None, device=None):
-    """t as a contiguous device tensor, checked; its address."""
-    if not (t.is_cuda and t.is_contiguous()) or (dtype is not None and t.dtype != dtype):
-        raise TypeError(f"{name} must be a contiguous {dtype or 'device'} tensor on a GPU")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _refuse(t, name, dtype, shape, dev):
+    if not t.is_cuda or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be a contiguous {dtype or ''} device tensor")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {list(shape)}, not {list(t.shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the input on {device}")
+    raise ValueError(f"{name} is on {t.device}, another tensor on device {dev}")
+
+
+def _ptr(t, name, dtype, shape, dev):
+    """The address of a contiguous tensor of this type and shape on device `dev` (None: any), checked.  0.3 us; the calls below have up to a
+    dozen tensors and a kernel behind them that may take 3."""
+    if (t.dtype is not dtype and dtype is not None) or (shape is not None and t.shape != shape) or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, dev)
     return t.data_ptr()
 
 
-def _opt(t, name, dtype, shape, device):
-    return None if t is None else _dev(t, name, dtype, shape, device)
+def _input(t, name):
+    """Address and device of the tensor that decides where a call runs."""
+    dev = t.get_device()
+    if dev < 0 or not t.is_contiguous():
+        _refuse(t, name, None, None, dev)
+    return t.data_ptr(), dev
 
 
-class _OnDevice:
-    """The calls launch on the device that is current: make it that of the tensors (nothing to do in the usual case)."""
+def _launch(fn, where, dev, stream, *args):
+    """fn(*args, stream) with the tensors' device current, on its current stream or on `stream`."""
+    torch = _torch
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
+    back = torch._C._cuda_getDevice()
+    if back == dev:
+        rc = fn(*args, s)
+    else:
+        torch.cuda.set_device(dev)
+        try:
+            rc = fn(*args, s)
+        finally:
+            torch.cuda.set_device(back)
+    if rc:
+        raise PromError(rc, where)
 
-    def __init__(self, device):
-        torch = _torch or _import_torch()
-        torch.cuda._lazy_init()
-        self.to = device.index
-        self.back = torch._C._cuda_getDevice()
 
-    def __enter__(self):
-        if self.to != self.back:
-            _torch.cuda.set_device(self.to)
-
-    def __exit__(self, *exc):
-        if self.to != self.back:
-            _torch.cuda.set_device(self.back)
-
-
-def _norm_rows(x, name="x"):
-    if x.dim() < 1 or x.numel() == 0:
-        raise ValueError(f"{name} must have rows and columns")
-    cols = x.shape[-1]
+def _norm_rows(x):
+    cols = x.shape[-1] if x.dim() else 0
+    if not cols or not x.numel():
+        raise ValueError("x must have rows and columns")
     return x.numel() // cols, cols
 
 
@@ -669,17 +678,15 @@ def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=No
     """Layer norm over the last dimension of x (float32, bfloat16 or float16; weight and bias float32 or None).
     Returns (y, mean, rstd); mean and rstd float32, one per row."""
     torch = _torch or _import_torch()
-    px, d = _dev(x, "x"), x.device
+    px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
-    f32 = torch.float32
+    f32, by_row, by_col = torch.float32, (rows,), (cols,)
     y = torch.empty_like(x) if y is None else y
-    mean = torch.empty(rows, dtype=f32, device=d) if mean is None else mean
-    rstd = torch.empty(rows, dtype=f32, device=d) if rstd is None else rstd
-    with _OnDevice(d):
-        _check(load_library().prom_layernorm(
-            px, _type_of(x.dtype), rows, cols, _opt(weight, "weight", f32, (cols,), d), _opt(bias, "bias", f32, (cols,), d), float(eps),
-            _dev(y, "y", x.dtype, x.shape, d), _dev(mean, "mean", f32, (rows,), d), _dev(rstd, "rstd", f32, (rows,), d), _stream_ptr(stream)),
-            "prom_layernorm")
+    mean = torch.empty(rows, dtype=f32, device=x.device) if mean is None else mean
+    rstd = torch.empty_like(mean) if rstd is None else rstd
+    _launch((_lib or load_library()).prom_layernorm, "prom_layernorm", dev, stream, px, _type_of(x.dtype), rows, cols,
+            None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
+            _ptr(y, "y", x.dtype, x.shape, dev), _ptr(mean, "mean", f32, by_row, dev), _ptr(rstd, "rstd", f32, by_row, dev))
     return y, mean, rstd
 
 
@@ -688,46 +695,46 @@ def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps
     """The same with every row quantised to int8.  Returns (q int8 of x's shape, step, mean, rstd): the real value is
     q * step, row by row."""
     torch = _torch or _import_torch()
-    px, d = _dev(x, "x"), x.device
+    px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
-    f32 = torch.float32
-    q = torch.empty(x.shape, dtype=torch.int8, device=d) if q is None else q
-    step = torch.empty(rows, dtype=f32, device=d) if step is None else step
-    mean = torch.empty(rows, dtype=f32, device=d) if mean is None else mean
-    rstd = torch.empty(rows, dtype=f32, device=d) if rstd is None else rstd
-    with _OnDevice(d):
-        _check(load_library().prom_layernorm_quant(
-            px, _type_of(x.dtype), rows, cols, _opt(weight, "weight", f32, (cols,), d), _opt(bias, "bias", f32, (cols,), d), float(eps),
-            float(quant_eps), _dev(q, "q", torch.int8, x.shape, d), _dev(step, "step", f32, (rows,), d), _dev(mean, "mean", f32, (rows,), d),
-            _dev(rstd, "rstd", f32, (rows,), d), _stream_ptr(stream)), "prom_layernorm_quant")
+    f32, by_row, by_col = torch.float32, (rows,), (cols,)
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if q is None else q
+    step = torch.empty(rows, dtype=f32, device=x.device) if step is None else step
+    mean = torch.empty_like(step) if mean is None else mean
+    rstd = torch.empty_like(step) if rstd is None else rstd
+    _launch((_lib or load_library()).prom_layernorm_quant, "prom_layernorm_quant", dev, stream, px, _type_of(x.dtype), rows, cols,
+            None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
+            quant_eps, _ptr(q, "q", torch.int8, x.shape, dev), _ptr(step, "step", f32, by_row, dev), _ptr(mean, "mean", f32, by_row, dev),
+            _ptr(rstd, "rstd", f32, by_row, dev))
     return q, step, mean, rstd
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(t, rows, cols) -> int:
+    return int(load_library().prom_layernorm_backward_workspace_size(t, rows, cols))
+
+
 def prom_layernorm_backward_workspace_size(dtype, rows: int, cols: int) -> int:
-    return int(load_library().prom_layernorm_backward_workspace_size(_type_of(dtype), rows, cols))
+    return _norm_workspace(_type_of(dtype), rows, cols)
 
 
 def prom_layernorm_backward(dy, x, weight, mean, rstd, want_dx: bool = True, want_dweight: bool = True, want_dbias: bool = True,
                             workspace=None, stream=None):
     """Gradients of prom_layernorm.  Returns (dx, dweight, dbias), None for what is not wanted."""
     torch = _torch or _import_torch()
-    px, d = _dev(x, "x"), x.device
+    px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
-    f32 = torch.float32
-    pdy = _dev(dy, "dy", x.dtype, x.shape, d)
+    f32, d, t, by_row = torch.float32, x.device, _type_of(x.dtype), (rows,)
     dx = torch.empty_like(x) if want_dx else None
     dweight = torch.empty(cols, dtype=f32, device=d) if want_dweight else None
     dbias = torch.empty(cols, dtype=f32, device=d) if want_dbias else None
-    lib = load_library()
-    t = _type_of(x.dtype)
     if workspace is None and (want_dweight or want_dbias):
-        workspace = torch.empty(lib.prom_layernorm_backward_workspace_size(t, rows, cols), dtype=torch.uint8, device=d)
-    with _OnDevice(d):
-        _check(lib.prom_layernorm_backward(
-            pdy, px, t, rows, cols, _opt(weight, "weight", f32, (cols,), d), _dev(mean, "mean", f32, (rows,), d), _dev(rstd, "rstd", f32, (rows,), d),
-            None if dx is None else dx.data_ptr(), None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
-            None if workspace is None else _dev(workspace, "workspace", device=d),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_layernorm_backward")
+        workspace = torch.empty(_norm_workspace(t, rows, cols), dtype=torch.uint8, device=d)
+    _launch((_lib or load_library()).prom_layernorm_backward, "prom_layernorm_backward", dev, stream, _ptr(dy, "dy", x.dtype, x.shape, dev), px, t, rows,
+            cols, None if weight is None else _ptr(weight, "weight", f32, (cols,), dev), _ptr(mean, "mean", f32, by_row, dev),
+            _ptr(rstd, "rstd", f32, by_row, dev), dx.data_ptr() if want_dx else None, dweight.data_ptr() if want_dweight else None,
+            dbias.data_ptr() if want_dbias else None, None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
     return dx, dweight, dbias
 
 
@@ -740,19 +747,20 @@ class Lora:
     scale: "torch.Tensor"
     index: "torch.Tensor"
 
-    def _c(self, n, cin, cout, device) -> _LoraC:
+    def _c(self, n, cin, cout, dev) -> _LoraC:
         torch = _torch or _import_torch()
         a, b = self.a, self.b
         if a.dim() != 3:
             raise ValueError("a must be [adapters, rank, cin]")
-        adapters, rank = a.shape[0], a.shape[1]
-        return _LoraC(_dev(a, "a", None, (adapters, rank, cin), device), _dev(b, "b", a.dtype, (adapters, rank, cout), device),
-                      _dev(self.scale, "scale", torch.float32, (adapters,), device), _dev(self.index, "index", torch.int32, (n,), device),
+        adapters, rank, _ = a.shape
+        return _LoraC(_ptr(a, "a", None, (adapters, rank, cin), dev), _ptr(b, "b", a.dtype, (adapters, rank, cout), dev),
+                      _ptr(self.scale, "scale", torch.float32, (adapters,), dev), _ptr(self.index, "index", torch.int32, (n,), dev),
                       adapters, rank, _type_of(a.dtype))
 
 
-def prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank) -> int:
-    return int(load_library().prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank))
+@functools.lru_cache(maxsize=256)
+def prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank, has_hid: bool = False) -> int:
+    return int(load_library().prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank, int(has_hid)))
 
 
 def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora, dtype=None, y=None, hid=None, want_hid: bool = False,
@@ -760,30 +768,38 @@ def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora,
     """x int8 [n,h,w,cin] device, x_step float32 [n], w_scale float32 [cout], bias float32 [cout] or None.  y is of `dtype`: the adapters' type (default)
     or float32.  Returns y, or (y, hid float32 [n*h*w, rank]) with want_hid or a hid of the caller's."""
     torch = _torch or _import_torch()
-    _dev_i8(x, "x")
-    d = x.device
+    px, dev = _input(x, "x")
+    if x.dtype is not torch.int8:
+        raise TypeError("x must be a contiguous int8 device tensor")
     n, h, w, cin = x.shape
-    lc = lora._c(n, cin, cout, d)
-    f32 = torch.float32
+    lc = lora._c(n, cin, cout, dev)
+    f32, d = torch.float32, x.device
     if y is None:
         y = torch.empty((n, h, w, cout), dtype=dtype or lora.a.dtype, device=d)
-    want_hid = want_hid or hid is not None
-    if want_hid and hid is None:
+        py = y.data_ptr()
+    else:
+        py = _ptr(y, "y", None, (n, h, w, cout), dev)
+    if hid is not None:
+        want_hid, phid = True, _ptr(hid, "hid", f32, (n * h * w, lc.rank), dev)
+    elif want_hid:
         hid = torch.empty((n * h * w, lc.rank), dtype=f32, device=d)
-    lib = load_library()
+        phid = hid.data_ptr()
+    else:
+        phid = None
     if workspace is None:
-        workspace = torch.empty(lib.prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank), dtype=torch.uint8, device=d)
+        size = prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank, want_hid)
+        workspace = torch.empty(size, dtype=torch.uint8, device=d) if size else None
     if w_packed.numel() * w_packed.element_size() < cout * ((cin + 15) // 16) * 4:
         raise ValueError("w_packed is smaller than the packed form of [cout, cin]")
-    with _OnDevice(d):
-        _check(lib.prom_pw_conv_lora(
-            x.data_ptr(), n, h, w, cin, _dev(w_packed, "w_packed", device=d), int(cout), _dev(x_step, "x_step", f32, (n,), d),
-            _dev(w_scale, "w_scale", f32, (cout,), d), _opt(bias, "bias", f32, (cout,), d), ctypes.byref(lc), _dev(y, "y", None, (n, h, w, cout), d),
-            _type_of(y.dtype), _opt(hid, "hid", f32, (n * h * w, lc.rank), d), _dev(workspace, "workspace", device=d),
-            workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_pw_conv_lora")
+    _launch((_lib or load_library()).prom_pw_conv_lora, "prom_pw_conv_lora", dev, stream, px, n, h, w, cin, _ptr(w_packed, "w_packed", None, None, dev),
+            cout, _ptr(x_step, "x_step", f32, (n,), dev), _ptr(w_scale, "w_scale", f32, (cout,), dev),
+            None if bias is None else _ptr(bias, "bias", f32, (cout,), dev), lc, py, _type_of(y.dtype), phid,
+            None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
     return (y, hid) if want_hid else y
 
 
+@functools.lru_cache(maxsize=256)
 def prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, adapters, rank, dtype) -> int:
     return int(load_library().prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, adapters, rank, _type_of(dtype)))
 
@@ -793,27 +809,26 @@ def prom_pw_conv_lora_backward(dy, x, x_step, wt_packed, w_scale, lora: Lora, hi
     """Gradients of prom_pw_conv_lora: dy [n,h,w,cout] float32 or of the adapters' type; wt_packed: prom_pack_ternary of the transposed weights
     [cin, cout].  Returns (dx of dy's type [n,h,w,cin], da, db float32 of the adapters' shapes), None for what is not wanted."""
     torch = _torch or _import_torch()
-    _dev_i8(x, "x")
-    d = x.device
+    px, dev = _input(x, "x")
+    if x.dtype is not torch.int8:
+        raise TypeError("x must be a contiguous int8 device tensor")
     n, h, w, cin = x.shape
     cout = dy.shape[-1]
-    lc = lora._c(n, cin, cout, d)
-    f32 = torch.float32
-    pdy, t = _dev(dy, "dy", None, (n, h, w, cout), d), _type_of(dy.dtype)
+    lc = lora._c(n, cin, cout, dev)
+    f32, d = torch.float32, x.device
     dx = torch.empty((n, h, w, cin), dtype=dy.dtype, device=d) if want_dx else None
-    da = torch.empty(lora.a.shape, dtype=f32, device=d) if want_da else None
-    db = torch.empty(lora.b.shape, dtype=f32, device=d) if want_db else None
-    lib = load_library()
+    da = torch.empty((lc.adapters, lc.rank, cin), dtype=f32, device=d) if want_da else None
+    db = torch.empty((lc.adapters, lc.rank, cout), dtype=f32, device=d) if want_db else None
     if workspace is None:
-        workspace = torch.empty(lib.prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank, t), dtype=torch.uint8, device=d)
+        workspace = torch.empty(prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank, dy.dtype), dtype=torch.uint8, device=d)
     if want_dx and wt_packed.numel() * wt_packed.element_size() < cin * ((cout + 15) // 16) * 4:
         raise ValueError("wt_packed is smaller than the packed form of [cin, cout]")
-    with _OnDevice(d):
-        _check(lib.prom_pw_conv_lora_backward(
-            pdy, t, x.data_ptr(), n, h, w, cin, _opt(wt_packed, "wt_packed", None, None, d), cout, _dev(x_step, "x_step", f32, (n,), d),
-            _opt(w_scale, "w_scale", f32, (cout,), d), ctypes.byref(lc), _opt(hid, "hid", f32, (n * h * w, lc.rank), d),
-            None if dx is None else dx.data_ptr(), None if da is None else da.data_ptr(), None if db is None else db.data_ptr(),
-            _dev(workspace, "workspace", device=d), workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "prom_pw_conv_lora_backward")
+    _launch((_lib or load_library()).prom_pw_conv_lora_backward, "prom_pw_conv_lora_backward", dev, stream, _ptr(dy, "dy", None, (n, h, w, cout), dev),
+            _type_of(dy.dtype), px, n, h, w, cin, None if wt_packed is None else _ptr(wt_packed, "wt_packed", None, None, dev), cout,
+            _ptr(x_step, "x_step", f32, (n,), dev), None if w_scale is None else _ptr(w_scale, "w_scale", f32, (cout,), dev), lc,
+            None if hid is None else _ptr(hid, "hid", f32, (n * h * w, lc.rank), dev), dx.data_ptr() if want_dx else None,
+            da.data_ptr() if want_da else None, db.data_ptr() if want_db else None, _ptr(workspace, "workspace", None, None, dev),
+            workspace.numel() * workspace.element_size())
     return dx, da, db
 
 
@@ -829,24 +844,24 @@ class AdamWTensor:
     sq_scale: "Optional[torch.Tensor]" = None
     copy: "Optional[torch.Tensor]" = None
 
-    def _c(self, device) -> _AdamWTensorC:
+    def _c(self, dev) -> _AdamWTensorC:
         torch = _torch or _import_torch()
         n = self.param.numel()
-        p, g = _dev(self.param, "param", device=device), _dev(self.grad, "grad", device=device)
+        p, g = _ptr(self.param, "param", None, None, dev), _ptr(self.grad, "grad", None, None, dev)
         if self.grad.numel() != n or (self.copy is not None and self.copy.numel() != n):
             raise ValueError("param, grad and copy must have the same size")
         bits = 8 if self.exp_avg.dtype == torch.int8 else 32
-        m = _dev(self.exp_avg, "exp_avg", torch.int8 if bits == 8 else torch.float32, device=device)
-        v = _dev(self.exp_avg_sq, "exp_avg_sq", torch.uint8 if bits == 8 else torch.float32, device=device)
+        m = _ptr(self.exp_avg, "exp_avg", torch.int8 if bits == 8 else torch.float32, None, dev)
+        v = _ptr(self.exp_avg_sq, "exp_avg_sq", torch.uint8 if bits == 8 else torch.float32, None, dev)
         if self.exp_avg.numel() != n or self.exp_avg_sq.numel() != n:
             raise ValueError("the moments must have the parameter's size")
         blocks = ((n + 255) // 256,)
         if bits == 8 and (self.avg_scale is None or self.sq_scale is None):
             raise ValueError("moments in 8 bits need avg_scale and sq_scale")
-        ms = _dev(self.avg_scale, "avg_scale", torch.float32, blocks, device) if bits == 8 else None
-        vs = _dev(self.sq_scale, "sq_scale", torch.float32, blocks, device) if bits == 8 else None
-        return _AdamWTensorC(p, g, m, v, ms, vs, _opt(self.copy, "copy", None, None, device), n, _type_of(self.param.dtype), _type_of(self.grad.dtype),
-                             _type_of(self.copy.dtype) if self.copy is not None else PROM_F32, bits)
+        ms = _ptr(self.avg_scale, "avg_scale", torch.float32, blocks, dev) if bits == 8 else None
+        vs = _ptr(self.sq_scale, "sq_scale", torch.float32, blocks, dev) if bits == 8 else None
+        return _AdamWTensorC(p, g, m, v, ms, vs, None if self.copy is None else _ptr(self.copy, "copy", None, None, dev), n, _type_of(self.param.dtype),
+                             _type_of(self.grad.dtype), PROM_F32 if self.copy is None else _type_of(self.copy.dtype), bits)
 
 
 class AdamWTensors:
@@ -858,9 +873,9 @@ class AdamWTensors:
         self._keep = list(tensors)
         if not self._keep:
             raise ValueError("no tensors")
-        self.device = self._keep[0].param.device
+        _, self._dev = _input(self._keep[0].param, "param")
         self.count = len(self._keep)
-        arr = (_AdamWTensorC * self.count)(*[t._c(self.device) for t in self._keep])
+        arr = (_AdamWTensorC * self.count)(*[t._c(self._dev) for t in self._keep])
         lib = load_library()
         self._plan = _AdamWPlanC()
         bad = ctypes.c_int(-1)
@@ -868,49 +883,47 @@ class AdamWTensors:
         rc = lib.prom_adamw_table(arr, self.count, host.ctypes.data, host.size, ctypes.byref(self._plan), ctypes.byref(bad))
         if rc != PROM_OK:
             raise PromError(rc, f"prom_adamw_table (tensor {bad.value})")
-        self._table = torch.from_numpy(host).to(self.device)
+        self._table = torch.from_numpy(host).to(self._keep[0].param.device)
+        self._table_ptr = self._table.data_ptr()
 
     def step(self, step, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
              grad_scale=None, stream=None):
         """step: the step's number, from 1 on, or an int32 device tensor that holds it (a captured step then follows it); lr: a number or a
         float32 device tensor; grad_scale: None or a float32 device tensor that every gradient is multiplied by."""
-        torch = _torch or _import_torch()
-        d = self.device
-        h = _AdamWHyperC(0.0, float(beta1), float(beta2), float(eps), float(weight_decay), 0, None, None, None)
+        torch = _torch
+        dev = self._dev
+        h = _AdamWHyperC(0.0, beta1, beta2, eps, weight_decay, 0, None, None, None)
         if isinstance(step, torch.Tensor):
-            h.step_dev = _dev(step, "step", torch.int32, None, d)
+            h.step_dev = _ptr(step, "step", torch.int32, None, dev)
         else:
             h.step = int(step)
         if isinstance(lr, torch.Tensor):
-            h.lr_dev = _dev(lr, "lr", torch.float32, None, d)
+            h.lr_dev = _ptr(lr, "lr", torch.float32, None, dev)
         else:
             h.lr = float(lr)
         if grad_scale is not None:
-            h.grad_scale = _dev(grad_scale, "grad_scale", torch.float32, None, d)
-        with _OnDevice(d):
-            _check(load_library().prom_adamw_step(self._table.data_ptr(), ctypes.byref(self._plan), ctypes.byref(h), _stream_ptr(stream)),
-                   "prom_adamw_step")
+            h.grad_scale = _ptr(grad_scale, "grad_scale", torch.float32, None, dev)
+        _launch(_lib.prom_adamw_step, "prom_adamw_step", dev, stream, self._table_ptr, self._plan, h)
 
     def moment_targets(self, targets):
         """targets: an (exp_avg, exp_avg_sq) pair of float32 tensors for every tensor.  What moments() takes."""
-        torch = _torch or _import_torch()
+        torch = _torch
         targets = list(targets)
         if len(targets) != self.count:
             raise ValueError(f"{self.count} pairs are needed")
         for (m, v), t in zip(targets, self._keep):
             for name, o in (("exp_avg", m), ("exp_avg_sq", v)):
-                _dev(o, name, torch.float32, None, self.device)
+                _ptr(o, name, torch.float32, None, self._dev)
                 if o.numel() != t.param.numel():
                     raise ValueError("a moment's target must have the parameter's size")
-        at = torch.tensor([[m.data_ptr() for m, _ in targets], [v.data_ptr() for _, v in targets]], dtype=torch.int64, device=self.device)
+        at = torch.tensor([[m.data_ptr() for m, _ in targets], [v.data_ptr() for _, v in targets]], dtype=torch.int64, device=self._table.device)
         return targets, at
 
     def moments(self, targets, stream=None):
         """The moments of every tensor in float32, into moment_targets(...)."""
         keep, at = targets
-        with _OnDevice(self.device):
-            _check(load_library().prom_adamw_moments(self._table.data_ptr(), ctypes.byref(self._plan), at[0].data_ptr(), at[1].data_ptr(),
-                                                     _stream_ptr(stream)), "prom_adamw_moments")
+        p = at.data_ptr()
+        _launch(_lib.prom_adamw_moments, "prom_adamw_moments", self._dev, stream, self._table_ptr, self._plan, p, p + 8 * self.count)
         return keep
 
 

@@ -66,34 +66,6 @@ __host__ __device__ inline void corrections(double lr, double wd, double b1, dou
     *inv_root2 = (float)(1.0 / sqrt(1.0 - power(b2, t)));
 }
 
-// 4 elements from place i of a tensor of n
-__device__ __forceinline__ void load4(const void *p, int type, long long i, long long n, float (&out)[4])
-{
-    const int have = (int)min(n - i, 4LL);
-    auto go = [&](auto t) __attribute__((always_inline)) {
-        Piece<decltype(t), 4> q;
-        q.load_some(static_cast<const decltype(t) *>(p) + i, have);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = (float)q.e[e];
-    };
-    if (type == PROM_F32) go(float{});
-    else if (type == PROM_BF16) go(bf16_t{});
-    else go(f16_t{});
-}
-__device__ __forceinline__ void store4(void *p, int type, long long i, long long n, const float (&v)[4])
-{
-    const int have = (int)min(n - i, 4LL);
-    auto go = [&](auto t) __attribute__((always_inline)) {
-        Piece<decltype(t), 4> q;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q.e[e] = (decltype(t))v[e];
-        q.store_some(static_cast<decltype(t) *>(p) + i, have);
-    };
-    if (type == PROM_F32) go(float{});
-    else if (type == PROM_BF16) go(bf16_t{});
-    else go(f16_t{});
-}
-
 // m and sqrt(v) of a lane's 4 codes
 __device__ __forceinline__ void decode_moments(const int8_t *c, const uint8_t *r, float ms, float vs, float (&m)[4], float (&root)[4])
 {
@@ -105,92 +77,122 @@ __device__ __forceinline__ void decode_moments(const int8_t *c, const uint8_t *r
     }
 }
 
-template <int BITS>
-__device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper &h, float decay, float step_size, float inv_root2, float gs,
-                                           long long base, int lane)
+template <typename T> __device__ __forceinline__ void load4(const T *p, long long i, int have, float (&out)[4])
 {
-    float p[kAdamUnits][4], g[kAdamUnits][4], m[kAdamUnits][4], v[kAdamUnits][4];
-    Piece<int8_t, 4> mc[kAdamUnits];
-    Piece<uint8_t, 4> vc[kAdamUnits];
-    float ms[kAdamUnits], vs[kAdamUnits];
+    Piece<T, 4> q;
+    q.load_some(as_global(p) + i, have);
 #pragma unroll
-    for (int u = 0; u < kAdamUnits; ++u) {
-        const long long i = base + u * kAdamBlock + 4 * lane;
-        if (base + u * kAdamBlock >= t.n) continue;
-        const int have = (int)min(t.n - i, 4LL);
-        load4(t.p, t.ptype, i, t.n, p[u]);
-        load4(t.g, t.gtype, i, t.n, g[u]);
-        if constexpr (BITS == 8) {
-            mc[u].load_some(static_cast<const int8_t *>(t.m) + i, have);
-            vc[u].load_some(static_cast<const uint8_t *>(t.v) + i, have);
-            const long long b = (base + u * kAdamBlock) / kAdamBlock;
-            ms[u] = t.ms[b];
-            vs[u] = t.vs[b];
-        } else {
-            load4(t.m, PROM_F32, i, t.n, m[u]);
-            load4(t.v, PROM_F32, i, t.n, v[u]);
+    for (int e = 0; e < 4; ++e) out[e] = (float)q.e[e];
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, long long i, int have, const float (&v)[4])
+{
+    Piece<T, 4> q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q.e[e] = (T)v[e];
+    q.store_some(as_global(p) + i, have);
+}
+
+struct AdamScalars {
+    float decay, step_size, inv_root2, grad_scale;
+};
+
+// The units of a wavefront from element `base` on; WHOLE: all of them lie in the tensor.
+template <int BITS, bool WHOLE, typename TP, typename TG>
+__device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper &h, const AdamScalars &k, long long base, int lane)
+{
+    constexpr int U = WHOLE ? kAdamUnits : 1;
+    for (int u0 = 0; u0 < kAdamUnits; u0 += U) {
+        const long long at = base + u0 * kAdamBlock;
+        if (!WHOLE && at >= t.n) return;
+        const int have = WHOLE ? 4 : (int)min(t.n - at - 4 * lane, 4LL);
+        float p[U][4], g[U][4], m[U][4], v[U][4];
+        Piece<int8_t, 4> mc[U];
+        Piece<uint8_t, 4> vc[U];
+        float ms[U], vs[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long i = at + u * kAdamBlock + 4 * lane;
+            load4(static_cast<const TG *>(t.g), i, have, g[u]);
+            if constexpr (BITS == 8) {
+                mc[u].load_some(as_global(static_cast<const int8_t *>(t.m)) + i, have);
+                vc[u].load_some(as_global(static_cast<const uint8_t *>(t.v)) + i, have);
+                ms[u] = as_global(t.ms)[at / kAdamBlock + u];
+                vs[u] = as_global(t.vs)[at / kAdamBlock + u];
+            } else {
+                load4(static_cast<const float *>(t.m), i, have, m[u]);
+                load4(static_cast<const float *>(t.v), i, have, v[u]);
+            }
+            load4(static_cast<const TP *>(t.p), i, have, p[u]);
         }
-    }
 #pragma unroll
-    for (int u = 0; u < kAdamUnits; ++u) {
-        const long long i = base + u * kAdamBlock + 4 * lane;
-        if (base + u * kAdamBlock >= t.n) continue;
-        const int have = (int)min(t.n - i, 4LL);
-        if constexpr (BITS == 8) {
-            decode_moments(mc[u].e, vc[u].e, ms[u], vs[u], m[u], v[u]);
+        for (int u = 0; u < U; ++u) {
+            const long long i = at + u * kAdamBlock + 4 * lane;
+            if constexpr (BITS == 8) {
+                decode_moments(mc[u].e, vc[u].e, ms[u], vs[u], m[u], v[u]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[u][e] = mul_f32(v[u][e], v[u][e]);
-        }
-        float root[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float ge = mul_f32(g[u][e], gs);
-            m[u][e] = add_f32(mul_f32(m[u][e], h.beta1), mul_f32(ge, h.omb1));
-            v[u][e] = add_f32(mul_f32(v[u][e], h.beta2), mul_f32(mul_f32(ge, h.omb2), ge));
-            root[e] = sqrt_f32(v[u][e]);
-            const float denom = add_f32(mul_f32(root[e], inv_root2), h.eps);
-            p[u][e] = sub_f32(mul_f32(p[u][e], decay), __fdiv_rn(mul_f32(m[u][e], step_size), denom));
-        }
-        store4(t.p, t.ptype, i, t.n, p[u]);
-        if (t.copy) store4(t.copy, t.ctype, i, t.n, p[u]);
-        if constexpr (BITS == 32) {
-            store4(t.m, PROM_F32, i, t.n, m[u]);
-            store4(t.v, PROM_F32, i, t.n, v[u]);
-        } else {
-            float mt = 0.0f, vt = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < have) {
-                    mt = bits_max(mt, fabsf(m[u][e]));
-                    vt = bits_max(vt, fabsf(root[e]));
-                }
-            mt = wave_max_bits(mt);
-            vt = wave_max_bits(vt);
-            // below 2^-100 the inverse could overflow: such a block is held as zeros.  An infinity or a NaN makes the
-            // scale NaN, and with it every moment of the block from the next step on, as it would in 32 bits for its element.
-            constexpr float tiny = 0x1p-100f, huge = 0x1.fffffep127f;
-            const float minv = mt < tiny ? 0.0f : __fdiv_rn(16129.0f, mt), vinv = vt < tiny ? 0.0f : __fdiv_rn(65025.0f, vt);
-            const bool mfine = mt <= huge, vfine = vt <= huge;
-            Piece<int8_t, 4> co;
-            Piece<uint8_t, 4> ro;
+                for (int e = 0; e < 4; ++e) v[u][e] = mul_f32(v[u][e], v[u][e]);
+            }
+            float root[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float c = fminf(rintf(sqrt_f32(mul_f32(fabsf(m[u][e]), minv))), 127.0f);
-                float r = fminf(rintf(sqrt_f32(mul_f32(root[e], vinv))), 255.0f);
-                r = root[e] > 0.0f && vinv > 0.0f ? fmaxf(r, 1.0f) : r;
-                co.e[e] = mfine ? (int8_t)(m[u][e] < 0.0f ? -(int)c : (int)c) : (int8_t)0;
-                ro.e[e] = vfine ? (uint8_t)(int)r : (uint8_t)0;
+                const float ge = mul_f32(g[u][e], k.grad_scale);
+                m[u][e] = add_f32(mul_f32(m[u][e], h.beta1), mul_f32(ge, h.omb1));
+                v[u][e] = add_f32(mul_f32(v[u][e], h.beta2), mul_f32(mul_f32(ge, h.omb2), ge));
+                root[e] = sqrt_f32(v[u][e]);
+                const float denom = add_f32(mul_f32(root[e], k.inv_root2), h.eps);
+                p[u][e] = sub_f32(mul_f32(p[u][e], k.decay), __fdiv_rn(mul_f32(m[u][e], k.step_size), denom));
             }
-            co.store_some(static_cast<int8_t *>(t.m) + i, have);
-            ro.store_some(static_cast<uint8_t *>(t.v) + i, have);
-            if (lane == 0) {
-                const long long b = (base + u * kAdamBlock) / kAdamBlock;
-                const float nan = __int_as_float(0x7fc00000);
-                t.ms[b] = !mfine ? nan : mt < tiny ? 0.0f : mul_f32(mt, 1.0f / 16129.0f);
-                t.vs[b] = !vfine ? nan : vt < tiny ? 0.0f : mul_f32(vt, 1.0f / 65025.0f);
+            store4(static_cast<TP *>(t.p), i, have, p[u]);
+            if (t.copy) {
+                if (t.ctype == PROM_BF16) store4(static_cast<bf16_t *>(t.copy), i, have, p[u]);
+                else if (t.ctype == PROM_F16) store4(static_cast<f16_t *>(t.copy), i, have, p[u]);
+                else store4(static_cast<float *>(t.copy), i, have, p[u]);
+            }
+            if constexpr (BITS == 32) {
+                store4(static_cast<float *>(t.m), i, have, m[u]);
+                store4(static_cast<float *>(t.v), i, have, v[u]);
+            } else {
+                float mt = 0.0f, vt = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < have) {
+                        mt = bits_max(mt, fabsf(m[u][e]));
+                        vt = bits_max(vt, fabsf(root[e]));
+                    }
+                mt = wave_max_bits(mt);
+                vt = wave_max_bits(vt);
+                // below 2^-100 the inverse could overflow: such a block is held as zeros.  An infinity or a NaN makes the
+                // scale NaN, and with it every moment of the block from the next step on, as it would in 32 bits for its element.
+                constexpr float tiny = 0x1p-100f, huge = 0x1.fffffep127f;
+                const float minv = mt < tiny ? 0.0f : __fdiv_rn(16129.0f, mt), vinv = vt < tiny ? 0.0f : __fdiv_rn(65025.0f, vt);
+                const bool mfine = mt <= huge, vfine = vt <= huge;
+                Piece<int8_t, 4> co;
+                Piece<uint8_t, 4> ro;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float c = fminf(rintf(sqrt_f32(mul_f32(fabsf(m[u][e]), minv))), 127.0f);
+                    float r = fminf(rintf(sqrt_f32(mul_f32(root[e], vinv))), 255.0f);
+                    r = root[e] > 0.0f && vinv > 0.0f ? fmaxf(r, 1.0f) : r;
+                    co.e[e] = mfine ? (int8_t)(m[u][e] < 0.0f ? -(int)c : (int)c) : (int8_t)0;
+                    ro.e[e] = vfine ? (uint8_t)(int)r : (uint8_t)0;
+                }
+                co.store_some(as_global(static_cast<int8_t *>(t.m)) + i, have);
+                ro.store_some(as_global(static_cast<uint8_t *>(t.v)) + i, have);
+                if (lane == 0) {
+                    const float nan = __int_as_float(0x7fc00000);
+                    as_global(t.ms)[at / kAdamBlock + u] = !mfine ? nan : mt < tiny ? 0.0f : mul_f32(mt, 1.0f / 16129.0f);
+                    as_global(t.vs)[at / kAdamBlock + u] = !vfine ? nan : vt < tiny ? 0.0f : mul_f32(vt, 1.0f / 65025.0f);
+                }
             }
         }
     }
+}
+
+template <typename F> __device__ __forceinline__ void by_type(int type, F f)
+{
+    if (type == PROM_F32) f(float{});
+    else if (type == PROM_BF16) f(bf16_t{});
+    else f(f16_t{});
 }
 
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamTensor *__restrict__ tensors, const int *__restrict__ owner, const AdamHyper h)
@@ -200,11 +202,22 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamTensor *__restrict
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long base = (long long)((int)blockIdx.x - t.first) * kAdamChunk + wave * kAdamUnits * kAdamBlock;
     if (base >= t.n) return;
-    float decay = h.decay, step_size = h.step_size, inv_root2 = h.inv_root2;
-    if (h.step || h.lr) corrections(h.lr ? (double)*h.lr : h.lr_h, h.wd, h.b1, h.b2, h.step ? *h.step : h.step_h, &decay, &step_size, &inv_root2);
-    const float gs = h.grad_scale ? *h.grad_scale : 1.0f;
-    if (t.bits == 8) adam_units<8>(t, h, decay, step_size, inv_root2, gs, base, lane);
-    else adam_units<32>(t, h, decay, step_size, inv_root2, gs, base, lane);
+    AdamScalars k{h.decay, h.step_size, h.inv_root2, h.grad_scale ? *h.grad_scale : 1.0f};
+    if (h.step || h.lr) corrections(h.lr ? (double)*h.lr : h.lr_h, h.wd, h.b1, h.b2, h.step ? *h.step : h.step_h, &k.decay, &k.step_size, &k.inv_root2);
+    const bool whole = base + kAdamUnits * kAdamBlock <= t.n;
+    by_type(t.ptype, [&](auto tp) {
+        by_type(t.gtype, [&](auto tg) {
+            using TP = decltype(tp);
+            using TG = decltype(tg);
+            if (t.bits == 8) {
+                if (whole) adam_units<8, true, TP, TG>(t, h, k, base, lane);
+                else adam_units<8, false, TP, TG>(t, h, k, base, lane);
+            } else {
+                if (whole) adam_units<32, true, TP, TG>(t, h, k, base, lane);
+                else adam_units<32, false, TP, TG>(t, h, k, base, lane);
+            }
+        });
+    });
 }
 
 // The moments of every tensor in float32: what a checkpoint holds.
@@ -217,28 +230,51 @@ __global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamTensor *__
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long base = (long long)((int)blockIdx.x - t.first) * kAdamChunk + wave * kAdamUnits * kAdamBlock;
+    if (base >= t.n) return;
+    auto units = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int U = WHOLE ? kAdamUnits : 1;
+        for (int u0 = 0; u0 < kAdamUnits; u0 += U) {
+            const long long at = base + u0 * kAdamBlock;
+            if (!WHOLE && at >= t.n) return;
+            const int have = WHOLE ? 4 : (int)min(t.n - at - 4 * lane, 4LL);
+            float m[U][4], v[U][4];
+            if (t.bits == 8) {
+                Piece<int8_t, 4> mc[U];
+                Piece<uint8_t, 4> vc[U];
+                float ms[U], vs[U];
 #pragma unroll
-    for (int u = 0; u < kAdamUnits; ++u) {
-        const long long b0 = base + u * kAdamBlock;
-        if (b0 >= t.n) return;
-        const long long i = b0 + 4 * lane;
-        float m[4], v[4];
-        if (t.bits == 8) {
-            const int have = (int)min(t.n - i, 4LL);
-            Piece<int8_t, 4> mc;
-            Piece<uint8_t, 4> vc;
-            mc.load_some(static_cast<const int8_t *>(t.m) + i, have);
-            vc.load_some(static_cast<const uint8_t *>(t.v) + i, have);
-            decode_moments(mc.e, vc.e, t.ms[b0 / kAdamBlock], t.vs[b0 / kAdamBlock], m, v);
+                for (int u = 0; u < U; ++u) {
+                    const long long i = at + u * kAdamBlock + 4 * lane;
+                    mc[u].load_some(as_global(static_cast<const int8_t *>(t.m)) + i, have);
+                    vc[u].load_some(as_global(static_cast<const uint8_t *>(t.v)) + i, have);
+                    ms[u] = as_global(t.ms)[at / kAdamBlock + u];
+                    vs[u] = as_global(t.vs)[at / kAdamBlock + u];
+                }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = mul_f32(v[e], v[e]);
-        } else {
-            load4(t.m, PROM_F32, i, t.n, m);
-            load4(t.v, PROM_F32, i, t.n, v);
+                for (int u = 0; u < U; ++u) {
+                    decode_moments(mc[u].e, vc[u].e, ms[u], vs[u], m[u], v[u]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[u][e] = mul_f32(v[u][e], v[u][e]);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const long long i = at + u * kAdamBlock + 4 * lane;
+                    load4(static_cast<const float *>(t.m), i, have, m[u]);
+                    load4(static_cast<const float *>(t.v), i, have, v[u]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long i = at + u * kAdamBlock + 4 * lane;
+                store4(mo, i, have, m[u]);
+                store4(vo, i, have, v[u]);
+            }
         }
-        store4(mo, PROM_F32, i, t.n, m);
-        store4(vo, PROM_F32, i, t.n, v);
-    }
+    };
+    if (base + kAdamUnits * kAdamBlock <= t.n) units(std::true_type{});
+    else units(std::false_type{});
 }
 
 // Table: [count] AdamTensor, then [chunks] int32 owners.

@@ -283,18 +283,32 @@ __global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__
     if (has) {
         const int8_t *xr = x + (size_t)row * K;
         const TA *lr = low + ((size_t)l * rank + r0) * K;
-#pragma unroll 4
-        for (int k = 8 * lane; k < K; k += 512) {
-            Piece<int8_t, 8> v;
-            v.load_some(xr + k, K - k);
-            Piece<TA, 8> w[RC];
+        // U steps of 512 channels at a time: with 8 a row of 4096 channels leaves in one go
+        constexpr int U = RC == 1 ? 8 : 4;
+        const int end = K & ~511;
+        auto steps = [&](auto whole, int k, int u) __attribute__((always_inline)) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            constexpr int N = WHOLE ? U : 1;
+            Piece<int8_t, 8> v[N];
+            Piece<TA, 8> w[N][RC];
 #pragma unroll
-            for (int c = 0; c < RC; ++c) w[c].load_some(lr + (size_t)(r0 + c < rank ? c : 0) * K + k, K - k);
+            for (int n = 0; n < N; ++n) {
+                const int k0 = k + 512 * (n < u ? n : 0) + 8 * lane;
+                v[n].load_some(xr + k0, WHOLE ? 8 : K - k0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+                for (int c = 0; c < RC; ++c) w[n][c].load_some(lr + (size_t)(r0 + c < rank ? c : 0) * K + k0, WHOLE ? 8 : K - k0);
+            }
 #pragma unroll
-                for (int c = 0; c < RC; ++c) s[c] += (float)v.e[e] * (float)w[c].e[e];
-        }
+            for (int n = 0; n < N; ++n) {
+                if (n >= u) break;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int c = 0; c < RC; ++c) s[c] += (float)v[n].e[e] * (float)w[n][c].e[e];
+            }
+        };
+        for (int k = 0; k < end; k += 512 * U) steps(std::true_type{}, k, min(U, (end - k) >> 9));
+        if (end < K) steps(std::false_type{}, end, 1);
     }
     const float f = step[row / hw];
 #pragma unroll
@@ -525,14 +539,26 @@ static int planes_of_type(int type) { return type == PROM_F32 ? 3 : type == PROM
 
 }  // namespace prom
 
-extern "C" size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank)
+namespace prom {
+static bool lora_sizes(int n, int h, int w, int cin, int cout, int adapters, int rank, long long *m)
+{
+    if (n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0 || adapters <= 0 || rank <= 0) return false;
+    if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || rank > kLoraMaxRank || adapters > kLoraMaxAdapters) return false;
+    const long long hw = (long long)h * w;
+    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return false;
+    *m = hw * n;
+    return true;
+}
+// Bytes the forward call looks at.
+static size_t lora_forward_bytes(long long m, const LoraSpace &s, bool has_hid) { return m <= kLoraFew && has_hid ? 0 : s.bytes; }
+}  // namespace prom
+
+extern "C" size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank, int has_hid)
 {
     using namespace prom;
-    if (n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0 || adapters <= 0 || rank <= 0) return 0;
-    if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || rank > kLoraMaxRank || adapters > kLoraMaxAdapters) return 0;
-    const long long hw = (long long)h * w;
-    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return 0;
-    return lora_space(hw * n, n, cin, cout, adapters, rank, false, 0).bytes;
+    long long m = 0;
+    if (!lora_sizes(n, h, w, cin, cout, adapters, rank, &m)) return 0;
+    return lora_forward_bytes(m, lora_space(m, n, cin, cout, adapters, rank, false, 0), has_hid != 0);
 }
 
 extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, const void *w_packed, int cout, const float *x_step,
@@ -546,9 +572,10 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     const int yb = type_bytes(y_type);
     if (misaligned(x_step, 4) || misaligned(w_scale, 4) || misaligned(bias, 4) || misaligned(y, yb) || misaligned(hid, 4)) return PROM_EINVAL;
     const LoraSpace s = lora_space(m, n, cin, cout, lora->adapters, lora->rank, false, 0);
-    if (!workspace || workspace_bytes < s.bytes || misaligned(workspace, 256)) return PROM_EWORKSPACE;
+    const size_t need = lora_forward_bytes(m, s, hid != nullptr);
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return PROM_EWORKSPACE;
     const size_t pool = (size_t)lora->adapters * lora->rank * 2;
-    const Range out[3] = {{y, (size_t)m * cout * yb}, {hid, (size_t)m * lora->rank * 4}, {workspace, s.bytes}};
+    const Range out[3] = {{y, (size_t)m * cout * yb}, {hid, (size_t)m * lora->rank * 4}, {need ? workspace : nullptr, need}};
     const Range in[9] = {{x, (size_t)m * cin}, {w_packed, prom_packed_size(cout, cin)}, {x_step, (size_t)n * 4}, {w_scale, (size_t)cout * 4},
                          {bias, (size_t)cout * 4}, {lora->a, pool * cin}, {lora->b, pool * cout}, {lora->scale, (size_t)lora->adapters * 4},
                          {lora->index, (size_t)n * 4}};
@@ -622,8 +649,9 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
 extern "C" size_t prom_pw_conv_lora_backward_workspace_size(int n, int h, int w, int cin, int cout, int adapters, int rank, int dy_type)
 {
     using namespace prom;
-    if (prom_pw_conv_lora_workspace_size(n, h, w, cin, cout, adapters, rank) == 0 || !type_bytes(dy_type)) return 0;
-    return lora_space((long long)n * h * w, n, cin, cout, adapters, rank, true, planes_of_type(dy_type)).bytes;
+    long long m = 0;
+    if (!lora_sizes(n, h, w, cin, cout, adapters, rank, &m) || !type_bytes(dy_type)) return 0;
+    return lora_space(m, n, cin, cout, adapters, rank, true, planes_of_type(dy_type)).bytes;
 }
 
 extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int8_t *x, int n, int h, int w, int cin, const void *wt_packed, int cout,

@@ -387,13 +387,15 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 }
 
 // ---- a few rows -----------------------------------------------------------------------------------------------
-// Up to 64 rows: a workgroup owns 16 channels and all rows, its 8 wavefronts share the input channels 256 at a time (16 bytes of
-// codes per lane, 64 channels each), the sums meet in LDS.  The low-rank term is one dot product over the ranks per output on the
-// vector ALU, every row with its own adapter.  Bound by latency, then by the adapters' bytes.
+// Up to 64 rows: a workgroup owns 16 channels and all rows, its 8 wavefronts share the input channels 256 at a time, the sums meet in LDS.
+// Four lanes read 64 bytes of a row (and 16 of a channel's codes) in one instruction: every row passes the texture addresser
+// in whole runs.  The low-rank term is one dot product over the ranks per output on the vector ALU, every row with its own adapter; its
+// operands are requested before the product, which they do not depend on.  Bound by latency, then by the adapters' bytes.
 template <typename TO, typename TA, int MT>
 __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a)
 {
     __shared__ v4i red[8][MT][64];
+    constexpr int RP = 16;  // ranks requested ahead
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -401,74 +403,98 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     const int n0 = logical_block_id() * 16;
     if (n0 >= a.Nc) return;
     const int K = a.K, KW = a.KW;
+
+    // what the thread will write: row tid / 8, channels n0 + 2 * (tid % 8) and the next
+    const int cc = 2 * (tid & 7), c = n0 + cc;
+    const bool out = tid < 8 * a.m && c < a.Nc;
+    const int row = min(tid >> 3, a.m - 1), channels = out ? a.Nc - c : 0;
+    const int el = a.hw == 1 ? row : row / a.hw;
+    const int l = a.index[el];
+    const bool has = out && l >= 0 && l < a.adapters;
+    const float st = a.step[el];
+    const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * a.Nc + c;
+    const float *hid = a.hid + (size_t)row * a.rank;
+    Piece<TA, 2> b[RP];
+    float h[RP];
+    float f = 0.0f;
+    Piece<float, 2> ws, bi;
+    ws.load_some(a.w_scale + c, channels);
+    bi.load_some(a.bias + c, a.bias ? channels : 0);
+    if (has) {
+        f = a.scale[l];
+#pragma unroll
+        for (int r = 0; r < RP; ++r) {
+            const int rr = min(r, a.rank - 1);
+            b[r].load_some(low + (size_t)rr * a.Nc, channels);
+            h[r] = hid[rr];
+        }
+    }
+
     const uint32_t *wrow = a.wq + (size_t)min(n0 + j, a.Nc - 1) * KW;
+    const int8_t *xrow[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xrow[i] = static_cast<const int8_t *>(a.x) + (size_t)min(16 * i + j, a.m - 1) * K;
     v4i acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
-    for (int k = 256 * wave; k < K; k += 2048) {
-        const int k0 = k + 64 * g;
-        const int have = KW - k0 / 16;
-        Piece<int, 4> w;
-        if (have >= 4) w.load(reinterpret_cast<const int *>(wrow + k0 / 16));
-        else
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w.e[e] = e < have ? (int)wrow[k0 / 16 + e] : 0;
+    auto steps = [&](auto whole, int k) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        uint32_t w[4];
         Piece<int8_t, 16> v[MT][4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int q = 0; q < 4; ++q) {
+            const int k0 = k + 64 * q + 16 * g;
+            w[q] = wrow[WHOLE ? k0 >> 4 : min(k0 >> 4, KW - 1)];  // (past the row's end it meets zeros)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                v[i][q].load_some(static_cast<const int8_t *>(a.x) + (size_t)min(16 * i + j, a.m - 1) * K + k0 + 16 * q, K - k0 - 16 * q);
+            for (int i = 0; i < MT; ++i) v[i][q].load_some(xrow[i] + k0, WHOLE ? 16 : K - k0);
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const v4i A = decode_word_64((uint32_t)w.e[q]);
+            const v4i A = decode_word_64(w[q]);
 #pragma unroll
             for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[i][q]), acc[i], 0, 0, 0);
         }
-    }
+    };
+    const int end = K & ~255;
+    for (int k = 256 * wave; k < end; k += 2048) steps(std::true_type{}, k);
+    if (end < K && (end >> 8 & 7) == wave) steps(std::false_type{}, end);
 #pragma unroll
     for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
     __syncthreads();
-    // thread: row tid / 8, channels n0 + 2 * (tid % 8) and the next
-    const int row = tid >> 3, cc = 2 * (tid & 7);
-    if (row >= a.m || row >= 16 * MT) return;
+    if (!out) return;
     int s0 = 0, s1 = 0;
     {
-        const int i = row >> 4, from = (row & 15) + 16 * (cc >> 2), e = cc & 3;
+        const int from = (row & 15) + 16 * (cc >> 2), e = cc & 3;
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
-            const int *p = reinterpret_cast<const int *>(&red[w][i][from]) + e;
+            const int *p = reinterpret_cast<const int *>(&red[w][row >> 4][from]) + e;
             s0 += p[0];
             s1 += p[1];
         }
     }
-    const int c = n0 + cc;
-    if (c >= a.Nc) return;
-    const bool two = c + 1 < a.Nc;
-    const int el = a.hw == 1 ? row : row / a.hw;
-    const float st = a.step[el];
-    float z0 = base_value(s0, a.w_scale[c], st, a.bias ? a.bias[c] : 0.0f);
-    float z1 = two ? base_value(s1, a.w_scale[c + 1], st, a.bias ? a.bias[c + 1] : 0.0f) : 0.0f;
-    const int l = a.index[el];
-    if (l >= 0 && l < a.adapters) {
-        const TA *low = static_cast<const TA *>(a.low) + (size_t)l * a.rank * a.Nc + c;
-        const float *h = a.hid + (size_t)row * a.rank;
+    float z0 = base_value(s0, ws.e[0], st, bi.e[0]), z1 = base_value(s1, ws.e[1], st, bi.e[1]);
+    if (has) {
         float l0 = 0.0f, l1 = 0.0f;
-#pragma unroll 8
-        for (int r = 0; r < a.rank; ++r) {
-            Piece<TA, 2> b;
-            b.load_some(low + (size_t)r * a.Nc, two ? 2 : 1);
-            l0 += h[r] * (float)b.e[0];
-            l1 += h[r] * (float)b.e[1];
+#pragma unroll
+        for (int r = 0; r < RP; ++r) {
+            const float v = r < a.rank ? h[r] : 0.0f;
+            l0 += r < a.rank ? v * (float)b[r].e[0] : 0.0f;
+            l1 += r < a.rank ? v * (float)b[r].e[1] : 0.0f;
         }
-        const float f = a.scale[l];
+#pragma unroll 16
+        for (int r = RP; r < a.rank; ++r) {
+            Piece<TA, 2> v;
+            v.load_some(low + (size_t)r * a.Nc, channels);
+            l0 += hid[r] * (float)v.e[0];
+            l1 += hid[r] * (float)v.e[1];
+        }
         z0 += f * l0;
         z1 += f * l1;
     }
     Piece<TO, 2> o;
     o.e[0] = (TO)z0;
     o.e[1] = (TO)z1;
-    o.store_some(static_cast<TO *>(a.y) + (size_t)row * a.Nc + c, two ? 2 : 1);
+    o.store_some(static_cast<TO *>(a.y) + (size_t)row * a.Nc + c, channels);
 }
 
 // ---- launch ----------------------------------------------------------------------------------------------------

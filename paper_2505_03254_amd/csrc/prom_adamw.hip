@@ -80,7 +80,7 @@ __device__ __forceinline__ void decode_moments(const int8_t *c, const uint8_t *r
 template <typename T> __device__ __forceinline__ void load4(const T *p, long long i, int have, float (&out)[4])
 {
     Piece<T, 4> q;
-    q.load_some(as_global(p) + i, have);
+    q.load_some((const Global<T> *)p + i, have);
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] = (float)q.e[e];
 }
@@ -89,7 +89,7 @@ template <typename T> __device__ __forceinline__ void store4(T *p, long long i, 
     Piece<T, 4> q;
 #pragma unroll
     for (int e = 0; e < 4; ++e) q.e[e] = (T)v[e];
-    q.store_some(as_global(p) + i, have);
+    q.store_some((Global<T> *)p + i, have);
 }
 
 struct AdamScalars {
@@ -114,10 +114,10 @@ __device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper 
             const long long i = at + u * kAdamBlock + 4 * lane;
             load4(static_cast<const TG *>(t.g), i, have, g[u]);
             if constexpr (BITS == 8) {
-                mc[u].load_some(as_global(static_cast<const int8_t *>(t.m)) + i, have);
-                vc[u].load_some(as_global(static_cast<const uint8_t *>(t.v)) + i, have);
-                ms[u] = as_global(t.ms)[at / kAdamBlock + u];
-                vs[u] = as_global(t.vs)[at / kAdamBlock + u];
+                mc[u].load_some((const Global<int8_t> *)t.m + i, have);
+                vc[u].load_some((const Global<uint8_t> *)t.v + i, have);
+                ms[u] = ((Global<float> *)t.ms)[at / kAdamBlock + u];
+                vs[u] = ((Global<float> *)t.vs)[at / kAdamBlock + u];
             } else {
                 load4(static_cast<const float *>(t.m), i, have, m[u]);
                 load4(static_cast<const float *>(t.v), i, have, v[u]);
@@ -133,12 +133,23 @@ __device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper 
                 for (int e = 0; e < 4; ++e) v[u][e] = mul_f32(v[u][e], v[u][e]);
             }
             float root[4];
+            bool small = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float ge = mul_f32(g[u][e], k.grad_scale);
                 m[u][e] = add_f32(mul_f32(m[u][e], h.beta1), mul_f32(ge, h.omb1));
                 v[u][e] = add_f32(mul_f32(v[u][e], h.beta2), mul_f32(mul_f32(ge, h.omb2), ge));
-                root[e] = sqrt_f32(v[u][e]);
+                small |= v[u][e] < 0x1p-96f && v[u][e] > 0.0f;
+            }
+            if (__ballot(small)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) root[e] = sqrt_f32(v[u][e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) root[e] = sqrt_large_f32(v[u][e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
                 const float denom = add_f32(mul_f32(root[e], k.inv_root2), h.eps);
                 p[u][e] = sub_f32(mul_f32(p[u][e], k.decay), __fdiv_rn(mul_f32(m[u][e], k.step_size), denom));
             }
@@ -170,18 +181,19 @@ __device__ __forceinline__ void adam_units(const AdamTensor &t, const AdamHyper 
                 Piece<uint8_t, 4> ro;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float c = fminf(rintf(sqrt_f32(mul_f32(fabsf(m[u][e]), minv))), 127.0f);
-                    float r = fminf(rintf(sqrt_f32(mul_f32(root[e], vinv))), 255.0f);
+                    // (the root of a smaller argument than 2^-96 rounds to 0 however exact it is)
+                    const float c = fminf(rintf(sqrt_large_f32(mul_f32(fabsf(m[u][e]), minv))), 127.0f);
+                    float r = fminf(rintf(sqrt_large_f32(mul_f32(root[e], vinv))), 255.0f);
                     r = root[e] > 0.0f && vinv > 0.0f ? fmaxf(r, 1.0f) : r;
                     co.e[e] = mfine ? (int8_t)(m[u][e] < 0.0f ? -(int)c : (int)c) : (int8_t)0;
                     ro.e[e] = vfine ? (uint8_t)(int)r : (uint8_t)0;
                 }
-                co.store_some(as_global(static_cast<int8_t *>(t.m)) + i, have);
-                ro.store_some(as_global(static_cast<uint8_t *>(t.v)) + i, have);
+                co.store_some((Global<int8_t> *)t.m + i, have);
+                ro.store_some((Global<uint8_t> *)t.v + i, have);
                 if (lane == 0) {
                     const float nan = __int_as_float(0x7fc00000);
-                    as_global(t.ms)[at / kAdamBlock + u] = !mfine ? nan : mt < tiny ? 0.0f : mul_f32(mt, 1.0f / 16129.0f);
-                    as_global(t.vs)[at / kAdamBlock + u] = !vfine ? nan : vt < tiny ? 0.0f : mul_f32(vt, 1.0f / 65025.0f);
+                    ((Global<float> *)t.ms)[at / kAdamBlock + u] = !mfine ? nan : mt < tiny ? 0.0f : mul_f32(mt, 1.0f / 16129.0f);
+                    ((Global<float> *)t.vs)[at / kAdamBlock + u] = !vfine ? nan : vt < tiny ? 0.0f : mul_f32(vt, 1.0f / 65025.0f);
                 }
             }
         }
@@ -246,10 +258,10 @@ __global__ __launch_bounds__(256) void adamw_moments_kernel(const AdamTensor *__
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const long long i = at + u * kAdamBlock + 4 * lane;
-                    mc[u].load_some(as_global(static_cast<const int8_t *>(t.m)) + i, have);
-                    vc[u].load_some(as_global(static_cast<const uint8_t *>(t.v)) + i, have);
-                    ms[u] = as_global(t.ms)[at / kAdamBlock + u];
-                    vs[u] = as_global(t.vs)[at / kAdamBlock + u];
+                    mc[u].load_some((const Global<int8_t> *)t.m + i, have);
+                    vc[u].load_some((const Global<uint8_t> *)t.v + i, have);
+                    ms[u] = ((Global<float> *)t.ms)[at / kAdamBlock + u];
+                    vs[u] = ((Global<float> *)t.vs)[at / kAdamBlock + u];
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {

@@ -16,13 +16,15 @@ typedef _Float16 f16_t;
 
 inline int type_bytes(int type) { return type == PROM_F32 ? 4 : type == PROM_BF16 || type == PROM_F16 ? 2 : 0; }
 
-// The same pointer, known to point to global memory (one that comes out of memory or of a struct of pointers may be anything
-// to the compiler, and a flat access waits for LDS too).
-template <typename T> __device__ __forceinline__ T *as_global(T *p) { return (T *)(__attribute__((address_space(1))) T *)p; }
+// A pointer known to point to global memory.  One that comes out of memory may point anywhere to the compiler, and its flat accesses
+// wait for LDS as well as for each other (AdamW, whose pointers stand in a table: 257 us with flat accesses, see adamw_kernel for without).
+template <typename T> using Global = T __attribute__((address_space(1)));
 
 // A piece of 16 (8, 4) bytes at an address that is aligned to its elements only: gfx950 loads and stores dwords at any
 // byte address, and the row of an odd width starts anywhere.
 template <typename T, int N> struct Piece {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    typedef Vec Loose __attribute__((aligned(sizeof(T))));
     struct __attribute__((packed, aligned(sizeof(T)))) Raw { T e[N]; };
     T e[N];
     __device__ __forceinline__ void load(const T *p)
@@ -31,6 +33,12 @@ template <typename T, int N> struct Piece {
 #pragma unroll
         for (int i = 0; i < N; ++i) e[i] = r.e[i];
     }
+    __device__ __forceinline__ void load(const Global<T> *p)
+    {
+        const Vec v = *reinterpret_cast<const Global<Loose> *>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = v[i];
+    }
     __device__ __forceinline__ void store(T *p) const
     {
         Raw r;
@@ -38,16 +46,26 @@ template <typename T, int N> struct Piece {
         for (int i = 0; i < N; ++i) r.e[i] = e[i];
         *reinterpret_cast<Raw *>(p) = r;
     }
+    __device__ __forceinline__ void store(Global<T> *p) const
+    {
+        Vec v;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = e[i];
+        *reinterpret_cast<Global<Loose> *>(p) = v;
+    }
     // the first `have` elements (have may be anything); the others read as zero and are not written
-    __device__ __forceinline__ void load_some(const T *p, int have)
+    template <typename P> __device__ __forceinline__ void load_some(P p, int have)
     {
         if (have >= N) load(p);
         else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) e[i] = i < have ? p[i] : (T)0.0f;
+            for (int i = 0; i < N; ++i) {
+                e[i] = (T)0.0f;
+                if (i < have) e[i] = p[i];
+            }
         }
     }
-    __device__ __forceinline__ void store_some(T *p, int have) const
+    template <typename P> __device__ __forceinline__ void store_some(P p, int have) const
     {
         if (have >= N) store(p);
         else {
@@ -78,6 +96,18 @@ __device__ __forceinline__ float sub_f32(float a, float b)
 
 // correctly rounded (the header's __fsqrt_rn is not)
 __device__ __forceinline__ float sqrt_f32(float a) { return __builtin_sqrtf(a); }
+
+// The same for 0, 2^-96 and above, infinities and NaN.  The instruction's result s is off by one step at most; with d and u
+// its neighbours, the root lies below the middle of d and s where d * s >= a (the middle's square is d * s and a quarter of
+// a step's square more), above that of s and u where s * u < a.  sqrt_f32 scales small arguments as well: 14 instructions against 9.
+__device__ __forceinline__ float sqrt_large_f32(float a)
+{
+    const float s = __builtin_amdgcn_sqrtf(a);
+    const float d = __int_as_float(__float_as_int(s) - 1), u = __int_as_float(__float_as_int(s) + 1);
+    const float below = __builtin_fmaf(-d, s, a), above = __builtin_fmaf(-u, s, a);
+    float r = below <= 0.0f ? d : s;
+    return above > 0.0f ? u : r;
+}
 
 // Sum and maximum over the 64 lanes, the same in every lane and the same from run to run.  Five steps inside rows
 // and between them by DPP, whose latency is that of an addition (a shuffle through LDS takes 64 cycles and more).

@@ -61,6 +61,9 @@ template <int PT, int NW> struct LoraGeom {
     static constexpr int WAVE = kCodeBytes > OUT ? kCodeBytes : OUT;
     static constexpr int LOWS = 16 * (TN * 2 + 16);  // factors of 16 ranks
     static_assert(2 * LOWS <= NW * WAVE, "two buffers of them fit the wavefronts' own places");
+    // steps of rows requested ahead in registers: a step of the large tile is 64 instructions of 16 cycles for each of two wavefronts, long
+    // enough for one; with smaller tiles a step ends long before the next one's loads arrive (32 x 128, 52 steps: 34 us with one)
+    static constexpr int D = PT == 8 ? 1 : PT == 4 ? 2 : 4;
     static constexpr int ROWS = 2 * SLAB + NW * WAVE;       // row, adapter, step of every row
     static constexpr int CHANS = ROWS + TM * 12;            // w_scale, bias of every channel
     static constexpr size_t LDS = (size_t)CHANS + TN * 8;
@@ -101,13 +104,16 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     const int whole = row_bytes >> 7;
     const int first = !PLANES && (row_bytes & 127) ? 1 : 0;
     const int steps = whole + first;
-    v4i xr[NQ];
-    auto load_x = [&](int q) __attribute__((always_inline)) {
-        const int at = 128 * (q - first) + 16 * piece;
+    constexpr int D = G::D;
+    v4i xring[D][NQ];  // step q in slot q % D
+    // (what is asked for behind the last step repeats it, and a row without a whole step reads the row numbers: neither is used.  A
+    // test around the loads would make the compiler wait for the newest instead of the one it needs)
+    auto load_x = [&](int q, v4i(&xr)[NQ]) __attribute__((always_inline)) {
+        const int at = 128 * max(min(q, steps - 1) - first, 0) + 16 * piece;
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) xr[i] = *reinterpret_cast<const v4i_u *>(as_global(src[i] + at));
+        for (int i = 0; i < NQ; ++i) xr[i] = *reinterpret_cast<const v4i_u *>(src[i] + at);
     };
-    auto put_x = [&](int slab) __attribute__((always_inline)) {
+    auto put_x = [&](int slab, const v4i(&xr)[NQ]) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) *reinterpret_cast<v4i *>(lds + slab * G::SLAB + (tid + G::NT * q) * 16) = xr[q];
     };
@@ -124,6 +130,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 #pragma unroll
     for (int r = 0; r < 4; ++r) wrow[r] = a.wq + (size_t)min(n0 + 16 * r + (lane >> 2), Nc - 1) * KW;
     v4i wr[4];
+    int wshift = 0;  // words that lie before the ones wanted: a row's last ones are read as the row's last four
     auto load_w = [&](int group) __attribute__((always_inline)) {
         const int q = min(GS * group + wpiece / WS, steps - 1);
         int ws = WS * (q < first ? whole : q - first) + wpiece % WS;
@@ -131,20 +138,23 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             if (ws >= wsteps) ws -= wsteps;
             if (ws >= wsteps) ws -= wsteps;
         }
-        if ((KW & 3) == 0) {
-            ws = min(ws, (KW >> 2) - 1);
+        const int from = max(min(4 * ws, KW - 4), 0);
+        wshift = min(4 * ws - from, 3);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(as_global(wrow[r] + 4 * ws));
-        } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) wr[r][e] = (int)as_global(wrow[r])[min(4 * ws + e, KW - 1)];
-        }
+        for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(wrow[r] + from);
     };
     unsigned char *wput = codes + wpiece * kCodeStep + (lane >> 2) * 16;
     const unsigned char *wget = codes + j * 16 + g * 4;
     auto put_w = [&]() __attribute__((always_inline)) {
+        if ((KW & 3) != 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const v4i v = wr[r];
+                const bool odd = wshift & 1, two = wshift & 2;
+                const int x0 = odd ? v[1] : v[0], x1 = odd ? v[2] : v[1], x2 = odd ? v[3] : v[2];
+                wr[r] = v4i{two ? x2 : x0, two ? v[3] : x1, x2, v[3]};
+            }
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) *reinterpret_cast<v4i *>(wput + 256 * r) = wr[r];
     };
@@ -158,46 +168,97 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     int *lrow = reinterpret_cast<int *>(lds + G::ROWS);  // [TM] row, [TM] adapter (kNone: none), [TM] step
     float *lstep = reinterpret_cast<float *>(lrow + 2 * G::TM);
     float *lws = reinterpret_cast<float *>(lds + G::CHANS);  // [TN] w_scale, [TN] bias
-    load_w(0);
-    for (int i = tid; i < G::TM; i += G::NT) {
-        const int row = a.rows[min(m0 + i, a.m - 1)];
-        const int el = a.hw == 1 ? row : row / a.hw;
-        const int l = a.index[el];
-        lrow[i] = row;
-        lrow[G::TM + i] = m0 + i < a.m && l >= 0 && l < a.adapters ? l : kNone;
-        if constexpr (!PLANES) lstep[i] = a.step[el];
+    if (KW >= 4) load_w(0);
+    else {  // one group holds every word of such a row; nothing behind it is used, and it is read from where there is something
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) wr[r][e] = (int)wrow[r][min(e, KW - 1)];
+            wrow[r] = reinterpret_cast<const uint32_t *>(a.rows);
+        }
     }
+    // What the epilogue needs first: a row's number, adapter and step by the thread that will bring its hid in (half tid & 1 of 16 ranks of
+    // row tid >> 1), a channel's scale and bias, and the first ranks of hid and of the first adapter's factors.  With small tiles the whole
+    // product takes no longer than these dependent loads, so they leave now and stay in registers; the large tile has none to spare.
+    constexpr bool EARLY = PT < 8;
+    constexpr int LP = G::TN * 2 + 16;  // bytes between ranks
+    const TA *low = static_cast<const TA *>(a.low);
+    Piece<TA, 8> lv[2];
+    auto load_low = [&](int l, int r0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int idx = tid + G::NT * q;
+            const int r = idx / (G::TN / 8), c = ntile * G::TN + idx % (G::TN / 8) * 8;
+            lv[q].load_some(low + ((size_t)l * a.rank + min(r0 + r, a.rank - 1)) * Nc + c, r0 + r < a.rank ? Nc - c : 0);
+        }
+    };
+    auto element = [&](int row) __attribute__((always_inline)) { return a.hw == 1 ? row : row / a.hw; };
+    const int hrow = tid >> 1, hhalf = tid & 1;
+    int my_row = a.rows[min(m0 + min(hrow, G::TM - 1), a.m - 1)];
+    int my_adapter = a.index[element(my_row)];
+    if (hrow >= G::TM || m0 + hrow >= a.m || my_adapter < 0 || my_adapter >= a.adapters) my_adapter = kNone;
+    int adapter0 = a.index[element(a.rows[m0])];  // the smallest one of the tile: its rows are sorted
+    if (adapter0 < 0 || adapter0 >= a.adapters) adapter0 = kNone;
+    float my_step = 0.0f, my_ws = 0.0f, my_bias = 0.0f, hscale = 1.0f;
     if constexpr (!PLANES) {
         const int c = min(ntile * G::TN + tid, Nc - 1);
-        lws[tid] = a.w_scale[c];
-        lws[G::TN + tid] = a.bias ? a.bias[c] : 0.0f;
+        my_step = a.step[element(my_row)];
+        my_ws = a.w_scale[c];
+        if (a.bias) my_bias = a.bias[c];
     }
+    auto put_info = [&]() __attribute__((always_inline)) {
+        if (hhalf == 0 && hrow < G::TM) {
+            lrow[hrow] = my_row;
+            lrow[G::TM + hrow] = my_adapter;
+            lstep[hrow] = my_step;
+        }
+        if constexpr (!PLANES) {
+            lws[tid] = my_ws;
+            lws[G::TN + tid] = my_bias;
+        }
+    };
+    Piece<float, 8> hv;
+    const float *hfrom = a.hid;
+    auto load_hid = [&](int r0) __attribute__((always_inline)) { hv.load_some(hfrom + r0, my_adapter != kNone ? a.rank - r0 - 8 * hhalf : 0); };
+    auto load_first = [&]() __attribute__((always_inline)) {
+        hfrom = a.hid + (size_t)my_row * a.rank + 8 * hhalf;
+        if (adapter0 == kNone) return;
+        load_hid(0);
+        if (a.scale && my_adapter != kNone) hscale = a.scale[my_adapter];
+        load_low(adapter0, 0);
+    };
+    if constexpr (!EARLY) put_info();
     if (first) {
         const int at = 128 * whole + 16 * piece;
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             Piece<int8_t, 16> v;
-            v.load_some(reinterpret_cast<const int8_t *>(as_global(src[q] + at)), row_bytes - at);
-            xr[q] = __builtin_bit_cast(v4i, v);
+            v.load_some(reinterpret_cast<const int8_t *>(src[q] + at), row_bytes - at);
+            xring[0][q] = __builtin_bit_cast(v4i, v);
+            if (whole == 0) src[q] = reinterpret_cast<const unsigned char *>(a.rows);
         }
     } else
-        load_x(0);
+        load_x(0, xring[0]);
+#pragma unroll
+    for (int d = 1; d < D; ++d) load_x(d, xring[d]);
     put_w();
     load_w(1);
-    put_x(0);
-    if (steps > 1) load_x(1);
+    put_x(0, xring[0]);
+    load_x(D, xring[0]);
+    if constexpr (EARLY) load_first();
     lds_only_barrier();
 
     const int sw = (j & 7);
-    for (int s = 0; s < steps; ++s) {
-        const unsigned char *slab = lds + (s & 1) * G::SLAB + j * 128;
+    auto step = [&](auto turn, int s) __attribute__((always_inline)) {  // turn = s % 4
+        const int TURN = turn, NEXT = (TURN + 1) % D;
+        const unsigned char *slab = lds + (TURN & 1) * G::SLAB + j * 128;
         uint32_t wc[WS][4];
 #pragma unroll
         for (int h = 0; h < WS; ++h)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) wc[h][t] = *reinterpret_cast<const uint32_t *>(wget + (WS * (s % GS) + h) * kCodeStep + 256 * t);
-        put_x((s + 1) & 1);
-        if (s + 2 < steps) load_x(s + 2);
+            for (int t = 0; t < 4; ++t) wc[h][t] = *reinterpret_cast<const uint32_t *>(wget + (WS * (TURN % GS) + h) * kCodeStep + 256 * t);
+        put_x((TURN + 1) & 1, xring[NEXT]);
+        load_x(s + 1 + D, xring[NEXT]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v4i B[PT];
@@ -217,11 +278,26 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
                 }
             }
         }
-        if (s % GS == GS - 1) {  // (LDS operations of a wavefront keep their order, and no other one reads these words)
+        if (TURN % GS == GS - 1) {  // (LDS operations of a wavefront keep their order, and no other one reads these words)
             put_w();
             load_w(s / GS + 2);
         }
         lds_only_barrier();
+    };
+    static_assert(4 % D == 0 && 4 % GS == 0, "the turns below");
+    int s = 0;
+    if constexpr (D == 1) {  // (the large tile's registers do not hold four steps' code: 142 us against 182)
+        for (; s < steps; ++s) step(s & 3, s);
+    } else {
+        for (; s + 4 <= steps; s += 4) {
+            step(std::integral_constant<int, 0>{}, s);
+            step(std::integral_constant<int, 1>{}, s + 1);
+            step(std::integral_constant<int, 2>{}, s + 2);
+            step(std::integral_constant<int, 3>{}, s + 3);
+        }
+        if (s < steps) step(std::integral_constant<int, 0>{}, s);
+        if (s + 1 < steps) step(std::integral_constant<int, 1>{}, s + 1);
+        if (s + 2 < steps) step(std::integral_constant<int, 2>{}, s + 2);
     }
 
     // ---- epilogue: lane (j, g), register e of tile (i, t): row 16i + j, channel n0 + 16t + 4g + e --------------------
@@ -230,17 +306,6 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     // factors [16 ranks][TN channels] into the codes' place; both have two buffers in turn, and the next ones are on their way in
     // registers while the last ones are used.
     using L = LowPlanes<TO, TA>;
-    constexpr int LP = G::TN * 2 + 16;  // bytes between ranks
-    const TA *low = as_global(static_cast<const TA *>(a.low));
-    Piece<TA, 8> lv[2];
-    auto load_low = [&](int l, int r0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int idx = tid + G::NT * q;
-            const int r = idx / (G::TN / 8), c = ntile * G::TN + idx % (G::TN / 8) * 8;
-            lv[q].load_some(low + ((size_t)l * a.rank + min(r0 + r, a.rank - 1)) * Nc + c, r0 + r < a.rank ? Nc - c : 0);
-        }
-    };
     auto put_low = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -248,6 +313,15 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             lv[q].store(reinterpret_cast<TA *>(lds + 2 * G::SLAB + buffer * G::LOWS + idx / (G::TN / 8) * LP) + idx % (G::TN / 8) * 8);
         }
     };
+    if constexpr (EARLY) {
+        put_info();
+        lds_only_barrier();
+    } else {
+        my_row = lrow[min(hrow, G::TM - 1)];
+        my_adapter = hrow < G::TM ? lrow[G::TM + hrow] : kNone;
+        adapter0 = __builtin_amdgcn_readfirstlane(lrow[G::TM]);
+        load_first();
+    }
     int own[PT];  // adapter of row 16i + j
 #pragma unroll
     for (int i = 0; i < PT; ++i) own[i] = lrow[G::TM + 16 * i + j];
@@ -259,18 +333,6 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, 64));
         return __builtin_amdgcn_readfirstlane(next);
     };
-    const int adapter0 = next_adapter(-1);  // (the same in every wavefront of the workgroup)
-    // this thread's share of hid: half tid & 1 of the 16 ranks of row tid >> 1
-    const int hrow = tid >> 1, hhalf = tid & 1;
-    const bool hmine = hrow < G::TM && lrow[G::TM + min(hrow, G::TM - 1)] != kNone;
-    const float *hfrom = as_global(a.hid) + (size_t)lrow[min(hrow, G::TM - 1)] * a.rank + 8 * hhalf;
-    Piece<float, 8> hv;
-    float hscale = 1.0f;
-    if (adapter0 != kNone) {
-        hv.load_some(hfrom, hmine ? a.rank - 8 * hhalf : 0);
-        if (a.scale && hmine) hscale = a.scale[lrow[G::TM + hrow]];
-        load_low(adapter0, 0);
-    }
     v4f z[PT][4];
     if constexpr (PLANES) {
 #pragma unroll
@@ -320,7 +382,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
                 if (after != kNone) load_low(after, r0);
                 else if (r0 + 16 < a.rank) {
                     load_low(adapter0, r0 + 16);
-                    hv.load_some(hfrom + r0 + 16, hmine ? a.rank - r0 - 16 - 8 * hhalf : 0);
+                    load_hid(r0 + 16);
                 }
                 v8bf A1[4], A2[L::SECOND ? 4 : 1], A3[L::THIRD ? 4 : 1];
                 const TA *factors = reinterpret_cast<const TA *>(lds + 2 * G::SLAB + buffer * G::LOWS + 8 * (g & 1) * LP) + 64 * wave + j;
@@ -365,7 +427,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     // out through the wavefront's own LDS: 16 rows x 64 channels at a time, rows in whole runs
     constexpr int PITCH = 64 * (int)sizeof(TO) + 16;
     constexpr int VE = 16 / sizeof(TO), PR = 64 / VE;  // elements of a piece, pieces of a row
-    TO *y = as_global(static_cast<TO *>(a.y));
+    TO *y = static_cast<TO *>(a.y);
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
 #pragma unroll
@@ -417,19 +479,6 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     Piece<TA, 2> b[RP];
     float h[RP];
     float f = 0.0f;
-    Piece<float, 2> ws, bi;
-    ws.load_some(a.w_scale + c, channels);
-    bi.load_some(a.bias + c, a.bias ? channels : 0);
-    if (has) {
-        f = a.scale[l];
-#pragma unroll
-        for (int r = 0; r < RP; ++r) {
-            const int rr = min(r, a.rank - 1);
-            b[r].load_some(low + (size_t)rr * a.Nc, channels);
-            h[r] = hid[rr];
-        }
-    }
-
     const uint32_t *wrow = a.wq + (size_t)min(n0 + j, a.Nc - 1) * KW;
     const int8_t *xrow[MT];
 #pragma unroll
@@ -437,27 +486,61 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     v4i acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
-    auto steps = [&](auto whole, int k) __attribute__((always_inline)) {
+    // N steps' loads leave before the first is used; `then` is called between the two
+    auto steps = [&](auto whole, auto count, int k, auto then) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;
-        uint32_t w[4];
-        Piece<int8_t, 16> v[MT][4];
+        constexpr int N = decltype(count)::value;
+        uint32_t w[N][4];
+        Piece<int8_t, 16> v[N][MT][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int k0 = k + 64 * q + 16 * g;
-            w[q] = wrow[WHOLE ? k0 >> 4 : min(k0 >> 4, KW - 1)];  // (past the row's end it meets zeros)
+        for (int s = 0; s < N; ++s)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) v[i][q].load_some(xrow[i] + k0, WHOLE ? 16 : K - k0);
-        }
+            for (int q = 0; q < 4; ++q) {
+                const int k0 = k + 2048 * s + 64 * q + 16 * g;
+                w[s][q] = wrow[WHOLE ? k0 >> 4 : min(k0 >> 4, KW - 1)];  // (past the row's end it meets zeros)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const v4i A = decode_word_64(w[q]);
+                for (int i = 0; i < MT; ++i) v[s][i][q].load_some(xrow[i] + k0, WHOLE ? 16 : K - k0);
+            }
+        then();
 #pragma unroll
-            for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[i][q]), acc[i], 0, 0, 0);
+        for (int s = 0; s < N; ++s)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const v4i A = decode_word_64(w[s][q]);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[s][i][q]), acc[i], 0, 0, 0);
+            }
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    Piece<float, 2> ws, bi;
+    auto adapters = [&]() __attribute__((always_inline)) {
+        ws.load_some(a.w_scale + c, channels);
+        bi.load_some(a.bias + c, a.bias ? channels : 0);
+        if (has) {
+            f = a.scale[l];
+#pragma unroll
+            for (int r = 0; r < RP; ++r) {
+                const int rr = min(r, a.rank - 1);
+                b[r].load_some(low + (size_t)rr * a.Nc, channels);
+                h[r] = hid[rr];
+            }
         }
     };
+    auto nothing = [] {};
     const int end = K & ~255;
-    for (int k = 256 * wave; k < end; k += 2048) steps(std::true_type{}, k);
-    if (end < K && (end >> 8 & 7) == wave) steps(std::false_type{}, end);
+    int k = 256 * wave;
+    if (k + 2048 < end) {
+        steps(std::true_type{}, Two{}, k, adapters);
+        k += 4096;
+    } else if (k < end) {
+        steps(std::true_type{}, One{}, k, adapters);
+        k += 2048;
+    } else
+        adapters();
+    for (; k < end; k += 2048) steps(std::true_type{}, One{}, k, nothing);
+    if (end < K && (end >> 8 & 7) == wave) steps(std::false_type{}, One{}, end, nothing);
 #pragma unroll
     for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
     __syncthreads();

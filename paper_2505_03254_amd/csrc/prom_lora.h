@@ -19,7 +19,6 @@ namespace prom {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef int v4i_u __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int kLoraTile = 32;        // sorted rows of a workgroup of the shrinking product
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraMaxChannels = 65536;  // |64 * acc| < 2^31 and |acc| < 2^24 exact in float32
 constexpr int kLoraMaxAdapters = 65535;
@@ -68,9 +67,9 @@ struct LoraPlan {
     int *order;    // [n] batch elements in sorted order
     int *rows;     // [m] row numbers in sorted order
     int2 *groups;  // [adapters + 1] first position, rows
-    int4 *tiles;   // [m / kLoraTile + adapters + 1] group, first position, rows, 0
-    int4 *chunks;  // [m / chunk + adapters + 1] the same in tiles of `chunk` rows
-    int chunk;
+    int4 *tiles;   // [m / tile + adapters + 1] group, first position, rows, 0
+    int4 *chunks;  // [m / chunk + adapters + 1] the same in tiles of `chunk` rows, or NULL
+    int tile, chunk;
 };
 
 struct LoraGemmArgs {

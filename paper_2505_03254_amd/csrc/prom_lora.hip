@@ -71,12 +71,12 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
         const int base = first / tile + l, end = (first + count) / tile + l + 1;
         for (int k = threadIdx.x; k < end - base; k += 1024) out[base + k] = int4{l, first + k * tile, max(0, min(tile, count - k * tile)), 0};
     };
-    cut(p.tiles, kLoraTile);
+    cut(p.tiles, p.tile);
     if (p.chunks) cut(p.chunks, p.chunk);
 }
 
 // ---- the shrinking product: rows of one adapter to `rank` numbers each -------------------------------------
-// A workgroup takes up to 32 sorted rows of one adapter; its 8 wavefronts share the channels in steps (64 of int8, 32 of
+// A workgroup takes up to 16 I sorted rows of one adapter; its 8 wavefronts share the channels in steps (64 of int8, 32 of
 // real input), every one with all of the rows and ranks, and their sums meet in LDS.  Bound by the activations' bytes and,
 // from rank 32 on, by the adapter's, which every workgroup reads from L2.  The backward form writes the activations of the next
 // product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as +-2 there), so that dy is read once for both.
@@ -104,14 +104,14 @@ __device__ __forceinline__ v8bf codes_to_bf16(const int8_t *c)
     return r;
 }
 
-template <bool BACK, typename TX, typename TA, int RT>
+template <bool BACK, typename TX, typename TA, int RT, int I>
 __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a)
 {
     constexpr int PA = planes_of<TA>();
     constexpr int PX = BACK ? planes_of<TX>() : 1;  // (codes: one plane)
     constexpr int KS = BACK ? 32 : 64;  // channels of a step
     constexpr int KL = KS / 4;          // of them a lane's
-    __shared__ v4f red[4][2 * RT][64];
+    __shared__ v4f red[4][I * RT][64];
     const int4 tile = a.tiles[blockIdx.x];
     const int l = tile.x, count = tile.z;
     if (count == 0) return;
@@ -121,10 +121,10 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     const bool has = l < a.adapters;
     const int K = a.K;
 
-    int row[2], elem[2];
-    bool in[2];
+    int row[I], elem[I];
+    bool in[I];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < I; ++i) {
         in[i] = 16 * i + j < count;
         const int pos = tile.y + min(16 * i + j, count - 1);
         const int e = pos / a.hw;
@@ -132,27 +132,27 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
         row[i] = elem[i] * a.hw + (pos - e * a.hw);
         if (wave == 0 && g == 0 && in[i]) a.rows[pos] = row[i];
     }
-    v4f acc[2][RT];
+    v4f acc[I][RT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[i][t] = v4f{0, 0, 0, 0};
 
     const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * K;
-    // U steps of loads leave together before the first of them is used: with 32 rows to a workgroup there are no more than
-    // 2 wavefronts on a SIMD to wait with (rank 32, 8192 x 4096: 20 us with one step at a time)
+    // U steps of loads leave together before the first of them is used: there are 2 to 4 wavefronts on a SIMD to wait with
+    // (rank 32, 8192 x 4096: 20 us with one step at a time)
     constexpr int U = RT <= 2 ? 4 : RT == 4 ? 2 : 1;
     auto steps = [&](auto whole, int k, int by, int u) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;
         constexpr int N = WHOLE ? U : 1;
-        Piece<TX, BACK ? 8 : 16> v[N][2];
+        Piece<TX, BACK ? 8 : 16> v[N][I];
         Piece<float, 8> ws[N];
         Piece<TA, 8> w[N][RT][KL / 8];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int k0 = k + (n < u ? n : 0) * by + KL * g;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
+            for (int i = 0; i < I; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
             if (BACK && a.planes) ws[n].load_some(a.w_scale + k0, WHOLE ? 8 : K - k0);
             if (has)
 #pragma unroll
@@ -166,11 +166,11 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
         for (int n = 0; n < N; ++n) {
             if (n >= u) break;
             const int k0 = k + n * by + KL * g;
-            v8bf bx[2][BACK ? PX : 2];
+            v8bf bx[I][BACK ? PX : 2];
             if constexpr (BACK) {
                 if (a.planes) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < I; ++i) {
                         Piece<bf16_t, 8> o[PX];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
@@ -188,10 +188,10 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) split_piece<PX>(v[n][i], bx[i]);
+                for (int i = 0; i < I; ++i) split_piece<PX>(v[n][i], bx[i]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < I; ++i) {
                     bx[i][0] = codes_to_bf16(v[n][i].e);
                     bx[i][1] = codes_to_bf16(v[n][i].e + 8);
                 }
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                     v8bf aw[PA];
                     split_piece<PA>(w[n][t][h], aw);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < I; ++i) {
                         if constexpr (BACK) {
 #pragma unroll
                             for (int p = 0; p < PA; ++p)
@@ -232,24 +232,24 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     // sums of the 8 wavefronts, always added in the same order
     if (wave >= 4)
 #pragma unroll
-        for (int c = 0; c < 2 * RT; ++c) red[wave - 4][c][lane] = acc[c & 1][c >> 1];
+        for (int c = 0; c < I * RT; ++c) red[wave - 4][c][lane] = acc[c % I][c / I];
     __syncthreads();
     if (wave < 4)
 #pragma unroll
-        for (int c = 0; c < 2 * RT; ++c) {
+        for (int c = 0; c < I * RT; ++c) {
             const v4f o = red[wave][c][lane];
-            red[wave][c][lane] = acc[c & 1][c >> 1] + o;
+            red[wave][c][lane] = acc[c % I][c / I] + o;
         }
     __syncthreads();
 #pragma unroll
-    for (int c0 = 0; c0 < 2 * RT; c0 += 8) {
+    for (int c0 = 0; c0 < I * RT; c0 += 8) {
         const int c = c0 + wave;
-        if (c >= 2 * RT) break;
+        if (c >= I * RT) break;
         const v4f s = (red[0][c][lane] + red[1][c][lane]) + (red[2][c][lane] + red[3][c][lane]);
-        const int i = c & 1, t = c >> 1;
-        const bool ok = i ? in[1] : in[0];
-        const int r0 = i ? row[1] : row[0];
-        const float step = a.step[i ? elem[1] : elem[0]];
+        const int i = c % I, t = c / I;
+        const bool ok = i ? in[I - 1] : in[0];
+        const int r0 = i ? row[I - 1] : row[0];
+        const float step = a.step[i ? elem[I - 1] : elem[0]];
         const float f = !has ? 0.0f : BACK ? a.scale[l] : step;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -468,6 +468,31 @@ static size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 // have to fill the chip; 256 rows give 8192 rows 32 chunks of 16 workgroups and more.
 constexpr int kLoraChunk = 256;
 
+template <typename F> static void by_adapter_type(int type, F f)
+{
+    if (type == PROM_BF16) f(bf16_t{});
+    else f(f16_t{});
+}
+template <typename F> static void by_real_type(int type, F f)
+{
+    if (type == PROM_F32) f(float{});
+    else by_adapter_type(type, f);
+}
+// Rows of a workgroup of the shrinking product.  Forward 32: every workgroup reads the adapter again, from rank 16 on as many bytes as
+// its activations are (8192 x 4096, rank 32: 15.6 us, with 16 rows 22.7).  Backward 16 up to rank 32, where the
+// activations are twice the bytes, written once more: more workgroups keep more of them on their way (rank 16: 36.7 us, with 32 rows 43.2).
+static int lora_tile(int rank, bool back) { return back && rank <= 32 ? 16 : 32; }
+// f(rank tiles of 16, row tiles of 16)
+template <typename F> static void by_rank(int rank, bool back, F f)
+{
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    if (rank <= 16) back ? f(One{}, One{}) : f(One{}, Two{});
+    else if (rank <= 32) back ? f(Two{}, One{}) : f(Two{}, Two{});
+    else if (rank <= 64) f(std::integral_constant<int, 4>{}, Two{});
+    else f(std::integral_constant<int, 8>{}, Two{});
+}
+
 struct LoraSpace {  // offsets into the workspace
     size_t order, rows, groups, tiles, chunks, hid, g, gs, planes, part_a, part_b, bytes;
     int ntiles, nchunks;
@@ -481,7 +506,7 @@ static LoraSpace lora_space(long long m, int n, int cin, int cout, int adapters,
         at += up256(b);
         return o;
     };
-    s.ntiles = (int)(m / kLoraTile) + adapters + 1;
+    s.ntiles = (int)(m / lora_tile(rank, back)) + adapters + 1;
     s.nchunks = (int)(m / kLoraChunk) + adapters + 1;
     s.order = take((size_t)n * 4);
     s.rows = take((size_t)m * 4);
@@ -511,25 +536,6 @@ static int lora_check(int n, int h, int w, int cin, int cout, const void *wq, co
     if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return PROM_EUNSUPPORTED;
     *m = hw * n;
     return PROM_OK;
-}
-
-template <typename F> static void by_adapter_type(int type, F f)
-{
-    if (type == PROM_BF16) f(bf16_t{});
-    else f(f16_t{});
-}
-template <typename F> static void by_real_type(int type, F f)
-{
-    if (type == PROM_F32) f(float{});
-    else by_adapter_type(type, f);
-}
-// f(rank tiles of 16) up to `most`
-template <typename F> static void by_rank(int rank, F f)
-{
-    if (rank <= 16) f(std::integral_constant<int, 1>{});
-    else if (rank <= 32) f(std::integral_constant<int, 2>{});
-    else if (rank <= 64) f(std::integral_constant<int, 4>{});
-    else f(std::integral_constant<int, 8>{});
 }
 
 // Up to this many rows run without sorting, on the kernels whose workgroups hold every row.
@@ -623,6 +629,7 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     p.rows = reinterpret_cast<int *>(ws + s.rows);
     p.groups = reinterpret_cast<int2 *>(ws + s.groups);
     p.tiles = reinterpret_cast<int4 *>(ws + s.tiles);
+    p.tile = lora_tile(lora->rank, false);
     hipLaunchKernelGGL(lora_plan_kernel, dim3((unsigned)lora->adapters + 1), dim3(1024), 0, st, lora->index, n, ga.hw, lora->adapters, p);
     LoraShrinkArgs sa{};
     sa.in = x;
@@ -637,8 +644,8 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     sa.rank = lora->rank;
     sa.adapters = lora->adapters;
     by_adapter_type(lora->type, [&](auto t) {
-        by_rank(lora->rank, [&](auto rt) {
-            hipLaunchKernelGGL((lora_shrink_kernel<false, int8_t, decltype(t), decltype(rt)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
+        by_rank(lora->rank, false, [&](auto rt, auto it) {
+            hipLaunchKernelGGL((lora_shrink_kernel<false, int8_t, decltype(t), decltype(rt)::value, decltype(it)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
         });
     });
     ga.rows = p.rows;
@@ -683,6 +690,7 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
     p.rows = reinterpret_cast<int *>(ws + s.rows);
     p.groups = reinterpret_cast<int2 *>(ws + s.groups);
     p.tiles = reinterpret_cast<int4 *>(ws + s.tiles);
+    p.tile = lora_tile(lora->rank, true);
     p.chunks = reinterpret_cast<int4 *>(ws + s.chunks);
     p.chunk = kLoraChunk;
     clear_hip_error();
@@ -705,12 +713,12 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
     sa.rank = lora->rank;
     sa.adapters = lora->adapters;
     by_adapter_type(lora->type, [&](auto t) {
-        by_rank(lora->rank, [&](auto rt) {
+        by_rank(lora->rank, true, [&](auto rt, auto it) {
             const dim3 grid((unsigned)s.ntiles), block(512);
             if (dy_type == PROM_F32)
-                hipLaunchKernelGGL((lora_shrink_kernel<true, float, decltype(t), decltype(rt)::value>), grid, block, 0, st, sa);
+                hipLaunchKernelGGL((lora_shrink_kernel<true, float, decltype(t), decltype(rt)::value, decltype(it)::value>), grid, block, 0, st, sa);
             else
-                hipLaunchKernelGGL((lora_shrink_kernel<true, decltype(t), decltype(t), decltype(rt)::value>), grid, block, 0, st, sa);
+                hipLaunchKernelGGL((lora_shrink_kernel<true, decltype(t), decltype(t), decltype(rt)::value, decltype(it)::value>), grid, block, 0, st, sa);
         });
     });
     if (dx) {

@@ -129,9 +129,13 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     const uint32_t *wrow[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) wrow[r] = a.wq + (size_t)min(n0 + 16 * r + (lane >> 2), Nc - 1) * KW;
-    v4i wr[4];
-    int wshift = 0;  // words that lie before the ones wanted: a row's last ones are read as the row's last four
-    auto load_w = [&](int group) __attribute__((always_inline)) {
+    // groups requested ahead: with small tiles a group of int8 lasts two short steps, and codes come from memory as late as rows do
+    constexpr int DW = D > 1 && !PLANES ? 2 : 1;
+    struct Words {
+        v4i v[4];
+        int shift;  // words that lie before the ones wanted: a row's last ones are read as the row's last four
+    } wring[DW];    // group q in slot q % DW
+    auto load_w = [&](int group, Words &w) __attribute__((always_inline)) {
         const int q = min(GS * group + wpiece / WS, steps - 1);
         int ws = WS * (q < first ? whole : q - first) + wpiece % WS;
         if constexpr (PLANES) {
@@ -139,24 +143,23 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             if (ws >= wsteps) ws -= wsteps;
         }
         const int from = max(min(4 * ws, KW - 4), 0);
-        wshift = min(4 * ws - from, 3);
+        w.shift = min(4 * ws - from, 3);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) wr[r] = *reinterpret_cast<const v4i_u *>(wrow[r] + from);
+        for (int r = 0; r < 4; ++r) w.v[r] = *reinterpret_cast<const v4i_u *>(wrow[r] + from);
     };
     unsigned char *wput = codes + wpiece * kCodeStep + (lane >> 2) * 16;
     const unsigned char *wget = codes + j * 16 + g * 4;
-    auto put_w = [&]() __attribute__((always_inline)) {
-        if ((KW & 3) != 0) {
+    auto put_w = [&](const Words &w) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const v4i v = wr[r];
-                const bool odd = wshift & 1, two = wshift & 2;
+        for (int r = 0; r < 4; ++r) {
+            v4i v = w.v[r];
+            if ((KW & 3) != 0) {
+                const bool odd = w.shift & 1, two = w.shift & 2;
                 const int x0 = odd ? v[1] : v[0], x1 = odd ? v[2] : v[1], x2 = odd ? v[3] : v[2];
-                wr[r] = v4i{two ? x2 : x0, two ? v[3] : x1, x2, v[3]};
+                v = v4i{two ? x2 : x0, two ? v[3] : x1, x2, v[3]};
             }
+            *reinterpret_cast<v4i *>(wput + 256 * r) = v;
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) *reinterpret_cast<v4i *>(wput + 256 * r) = wr[r];
     };
 
     Acc acc[PT][4];
@@ -168,15 +171,17 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     int *lrow = reinterpret_cast<int *>(lds + G::ROWS);  // [TM] row, [TM] adapter (kNone: none), [TM] step
     float *lstep = reinterpret_cast<float *>(lrow + 2 * G::TM);
     float *lws = reinterpret_cast<float *>(lds + G::CHANS);  // [TN] w_scale, [TN] bias
-    if (KW >= 4) load_w(0);
+    if (KW >= 4) load_w(0, wring[0]);
     else {  // one group holds every word of such a row; nothing behind it is used, and it is read from where there is something
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) wr[r][e] = (int)wrow[r][min(e, KW - 1)];
+            for (int e = 0; e < 4; ++e) wring[0].v[r][e] = (int)wrow[r][min(e, KW - 1)];
             wrow[r] = reinterpret_cast<const uint32_t *>(a.rows);
         }
+        wring[0].shift = 0;
     }
+    if constexpr (DW == 2) load_w(1, wring[1]);
     // What the epilogue needs first: a row's number, adapter and step by the thread that will bring its hid in (half tid & 1 of 16 ranks of
     // row tid >> 1), a channel's scale and bias, and the first ranks of hid and of the first adapter's factors.  With small tiles the whole
     // product takes no longer than these dependent loads, so they leave now and stay in registers; the large tile has none to spare.
@@ -241,8 +246,8 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         load_x(0, xring[0]);
 #pragma unroll
     for (int d = 1; d < D; ++d) load_x(d, xring[d]);
-    put_w();
-    load_w(1);
+    put_w(wring[0]);
+    load_w(DW, wring[0]);
     put_x(0, xring[0]);
     load_x(D, xring[0]);
     if constexpr (EARLY) load_first();
@@ -279,8 +284,9 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
             }
         }
         if (TURN % GS == GS - 1) {  // (LDS operations of a wavefront keep their order, and no other one reads these words)
-            put_w();
-            load_w(s / GS + 2);
+            Words &w = wring[(TURN / GS + 1) % DW];
+            put_w(w);
+            load_w(s / GS + 1 + DW, w);
         }
         lds_only_barrier();
     };
@@ -591,10 +597,15 @@ template <int PT, int NW, bool PLANES, typename TO, typename TA> static void gem
 
 template <bool PLANES, typename TO, typename TA> static void gemm_pick(const LoraGemmArgs &a, hipStream_t st)
 {
-    // the widest tile that still gives every compute unit a workgroup
+    // The largest tile that still gives every compute unit a workgroup (the largest of all two: it runs two at a time), measured
+    // (us, tiles 128x256 / 64x256 / 32x256 / 32x128, int8): 8192 x 4096 x 4096 118 / 133 / 165 / 193, 2048 x 4096 x 4096 47 / 39 / 51 / 61,
+    // 512 x 4096 x 4096 39 / 26 / 22 / 25, 128 x 4096 x 4096 45 / 28 / 21 / 20; up to 128 channels half of a wide tile is empty
+    // (12544 x 512 x 128: 16 / 11 / 11 / 10).
     auto tiles = [&](int tm, int tn) { return (long long)((a.m + tm - 1) / tm) * ((a.Nc + tn - 1) / tn); };
-    if (tiles(128, 256) >= 256) gemm_launch<8, 4, PLANES, TO, TA>(a, st);
-    else if (tiles(64, 128) >= 256) gemm_launch<4, 2, PLANES, TO, TA>(a, st);
+    if (a.Nc <= 128) gemm_launch<2, 2, PLANES, TO, TA>(a, st);
+    else if (tiles(128, 256) >= 512) gemm_launch<8, 4, PLANES, TO, TA>(a, st);
+    else if (tiles(64, 256) >= 256) gemm_launch<4, 4, PLANES, TO, TA>(a, st);
+    else if (tiles(32, 256) >= 256) gemm_launch<2, 4, PLANES, TO, TA>(a, st);
     else gemm_launch<2, 2, PLANES, TO, TA>(a, st);
 }
 

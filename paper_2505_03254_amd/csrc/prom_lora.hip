@@ -328,25 +328,31 @@ struct LoraGradArgs {
     const void *in;      // [m][C]
     const float *coef;   // [m][rank]
     const float *scale;  // [adapters] or NULL: factor of the coefficients
+    float *part;         // [chunks][rank][C]
+    float *out;          // [adapters][rank][C]
+    int C, blocks;       // blocks: workgroups of 512 columns, 0: not asked for
+};
+struct LoraGradBoth {    // da (int8 rows) and db share a launch: alone neither fills the chip
+    LoraGradArgs a, b;
     const int *rows;
     const int4 *chunks;
-    float *part;         // [chunks][rank][C]
-    int C, rank, adapters;
+    const int2 *groups;
+    int rank, adapters, chunk;
 };
 
 template <typename TX, int RT>
-__global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
+__device__ __forceinline__ void lora_grad_part(const LoraGradBoth &all, const LoraGradArgs &a, int block)
 {
     constexpr bool CODES = std::is_same<TX, int8_t>::value;
     constexpr int PX = CODES ? 1 : planes_of<TX>();
-    const int4 chunk = a.chunks[blockIdx.x];
-    if (chunk.z == 0 || chunk.x >= a.adapters) return;
+    const int4 chunk = all.chunks[blockIdx.x];
+    if (chunk.z == 0 || chunk.x >= all.adapters) return;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = lane & 15, g = lane >> 4;
-    const int c0 = (blockIdx.y * 4 + wave) * 128 + 8 * j;
+    const int c0 = (block * 4 + wave) * 128 + 8 * j;
     const int r0 = blockIdx.z * 16 * RT;
-    if ((int)(blockIdx.y * 4 + wave) * 128 >= a.C) return;
+    if ((block * 4 + wave) * 128 >= a.C) return;
     const float f = a.scale ? a.scale[chunk.x] : 1.0f;
 
     v4f acc[RT][8];
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
     auto all_rows = [&](auto whole) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;  // every step has 32 rows and every lane 8 columns
         auto load_rows = [&](int m, Piece<int, 8> &row) __attribute__((always_inline)) {
-            row.load_some(a.rows + chunk.y + m + 8 * g, WHOLE ? 8 : chunk.z - m - 8 * g);
+            row.load_some(all.rows + chunk.y + m + 8 * g, WHOLE ? 8 : chunk.z - m - 8 * g);
         };
         auto load = [&](int m, const Piece<int, 8> &row, Piece<TX, 8>(&v)[8], float(&c)[RT][8]) __attribute__((always_inline)) {
             const int have = WHOLE ? 8 : chunk.z - m - 8 * g;  // rows of this lane
@@ -370,7 +376,7 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     c[t][e] = 0.0f;
-                    if (e < have) c[t][e] = a.coef[(size_t)row.e[e] * a.rank + min(r0 + 16 * t + j, a.rank - 1)];
+                    if (e < have) c[t][e] = a.coef[(size_t)row.e[e] * all.rank + min(r0 + 16 * t + j, all.rank - 1)];
                 }
             }
         };
@@ -423,17 +429,17 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
             }
         }
     };
-    const int col = (int)(blockIdx.y * 4 + wave) * 128;
+    const int col = (block * 4 + wave) * 128;
     if ((chunk.z & 31) == 0 && col + 128 <= a.C) all_rows(std::true_type{});
     else all_rows(std::false_type{});
     // lane (j, g), register e of tile (t, c): rank 16t + 4g + e, column c0 + c
-    float *out = a.part + (size_t)blockIdx.x * a.rank * a.C;
+    float *out = a.part + (size_t)blockIdx.x * all.rank * a.C;
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = r0 + 16 * t + 4 * g + e;
-            if (r >= a.rank) continue;
+            if (r >= all.rank) continue;
             Piece<float, 8> o;
 #pragma unroll
             for (int c = 0; c < 8; ++c) o.e[c] = acc[t][c][e];
@@ -441,24 +447,35 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradArgs a)
         }
 }
 
-__global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float *__restrict__ part, const int2 *__restrict__ groups, float *__restrict__ out,
-                                                            int chunk, int rank, int C)
+template <typename TX, int RT>
+__global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradBoth all)
 {
+    if ((int)blockIdx.y < all.a.blocks) lora_grad_part<int8_t, RT>(all, all.a, blockIdx.y);
+    else lora_grad_part<TX, RT>(all, all.b, blockIdx.y - all.a.blocks);
+}
+
+__global__ __launch_bounds__(256) void lora_grad_sum_kernel(const LoraGradBoth all)
+{
+    const int na = all.a.blocks ? (all.a.C + 1023) / 1024 : 0;
+    const bool first = (int)blockIdx.y < na;
+    const LoraGradArgs &a = first ? all.a : all.b;
+    const int rank = all.rank, C = a.C;
     const int l = blockIdx.x / rank, r = blockIdx.x - l * rank;
-    const int c0 = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const int c0 = (((int)blockIdx.y - (first ? 0 : na)) * 256 + threadIdx.x) * 4;
     if (c0 >= C) return;
-    const int2 grp = groups[l];
-    const int base = grp.x / chunk + l, chunks = (grp.y + chunk - 1) / chunk;
+    const int2 grp = all.groups[l];
+    const int base = grp.x / all.chunk + l, chunks = (grp.y + all.chunk - 1) / all.chunk;
     Piece<float, 4> s;
 #pragma unroll
     for (int e = 0; e < 4; ++e) s.e[e] = 0.0f;
+#pragma unroll 4
     for (int k = 0; k < chunks; ++k) {
         Piece<float, 4> v;
-        v.load_some(part + ((size_t)(base + k) * rank + r) * C + c0, C - c0);
+        v.load_some(a.part + ((size_t)(base + k) * rank + r) * C + c0, C - c0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s.e[e] += v.e[e];
     }
-    s.store_some(out + ((size_t)l * rank + r) * C + c0, C - c0);
+    s.store_some(a.out + ((size_t)l * rank + r) * C + c0, C - c0);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -741,21 +758,25 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
         ga.Kp = sa.Kp;
         lora_gemm(ga, lora->type, dy_type, true, st);
     }
-    auto grad = [&](const void *in, int in_type, const float *coef, const float *scale, float *part, float *dst, int C) {
-        LoraGradArgs g{in, coef, scale, p.rows, p.chunks, part, C, lora->rank, lora->adapters};
-        auto go = [&](auto t) {
-            const unsigned cols = (unsigned)((C + 511) / 512);
+    if (da || db) {
+        LoraGradBoth all{};
+        if (da) all.a = {x, sa.out_step, nullptr, reinterpret_cast<float *>(ws + s.part_a), da, cin, (cin + 511) / 512};
+        if (db) all.b = {dy, hid, lora->scale, reinterpret_cast<float *>(ws + s.part_b), db, cout, (cout + 511) / 512};
+        all.rows = p.rows;
+        all.chunks = p.chunks;
+        all.groups = p.groups;
+        all.rank = lora->rank;
+        all.adapters = lora->adapters;
+        all.chunk = kLoraChunk;
+        by_real_type(dy_type, [&](auto t) {
+            const unsigned cols = (unsigned)(all.a.blocks + all.b.blocks);
             if (lora->rank <= 16)
-                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 1>), dim3((unsigned)s.nchunks, cols, 1), dim3(256), 0, st, g);
+                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 1>), dim3((unsigned)s.nchunks, cols, 1), dim3(256), 0, st, all);
             else
-                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 2>), dim3((unsigned)s.nchunks, cols, (unsigned)((lora->rank + 31) / 32)), dim3(256), 0, st, g);
-        };
-        if (in_type < 0) go(int8_t{});
-        else by_real_type(in_type, go);
-        hipLaunchKernelGGL(lora_grad_sum_kernel, dim3((unsigned)(lora->adapters * lora->rank), (unsigned)((C + 1023) / 1024)), dim3(256), 0, st, part, p.groups,
-                           dst, kLoraChunk, lora->rank, C);
-    };
-    if (da) grad(x, -1, sa.out_step, nullptr, reinterpret_cast<float *>(ws + s.part_a), da, cin);
-    if (db) grad(dy, dy_type, hid, lora->scale, reinterpret_cast<float *>(ws + s.part_b), db, cout);
+                hipLaunchKernelGGL((lora_grad_kernel<decltype(t), 2>), dim3((unsigned)s.nchunks, cols, (unsigned)((lora->rank + 31) / 32)), dim3(256), 0, st, all);
+        });
+        hipLaunchKernelGGL(lora_grad_sum_kernel, dim3((unsigned)(lora->adapters * lora->rank), (unsigned)((da ? (cin + 1023) / 1024 : 0) + (db ? (cout + 1023) / 1024 : 0))),
+                           dim3(256), 0, st, all);
+    }
     return check_launch();
 }

@@ -51,8 +51,8 @@ constexpr int kNone = 0x7fffffff;  // the adapter of rows without one
 constexpr int kCodeStep = 64 * 16 + 32;  // a wavefront's words of a word step: [64 channels][4 words]
 constexpr int kCodeBytes = 4 * kCodeStep;
 
-template <int PT, int NW> struct LoraGeom {
-    static constexpr int NT = 64 * NW;
+template <int PT, int NW, int KG> struct LoraGeom {
+    static constexpr int NT = 64 * NW;                      // threads of a group
     static constexpr int TM = 16 * PT;
     static constexpr int TN = 64 * NW;
     static constexpr int NQ = TM * 8 / NT;  // 16-byte pieces of a step per thread
@@ -64,22 +64,27 @@ template <int PT, int NW> struct LoraGeom {
     // steps of rows requested ahead in registers: a step of the large tile is 64 instructions of 16 cycles for each of two wavefronts, long
     // enough for one; with smaller tiles a step ends long before the next one's loads arrive (32 x 128, 52 steps: 34 us with one)
     static constexpr int D = PT == 8 ? 1 : PT == 4 ? 2 : 4;
-    static constexpr int ROWS = 2 * SLAB + NW * WAVE;       // row, adapter, step of every row
+    static constexpr int GROUP = 2 * SLAB + NW * WAVE;      // LDS of a group: slabs, then the wavefronts' own places
+    static_assert(KG == 1 || PT * 4 * 1024 * NW <= GROUP, "a group's sums fit its place");
+    static constexpr int ROWS = KG * GROUP;                 // row, adapter, step of every row
     static constexpr int CHANS = ROWS + TM * 12;            // w_scale, bias of every channel
     static constexpr size_t LDS = (size_t)CHANS + TN * 8;
 };
 
 // PLANES: bf16 planes instead of int8 (aligned and padded by their writer).
-template <int PT, int NW, bool PLANES, typename TO, typename TA>
-__global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArgs a, int ntiles)
+// KG groups of NW wavefronts share the steps of a tile, each with slabs and codes of its own; their sums meet in LDS, and the first group goes on.
+template <int PT, int NW, int KG, bool PLANES, typename TO, typename TA>
+__global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGemmArgs a, int ntiles)
 {
-    using G = LoraGeom<PT, NW>;
+    using G = LoraGeom<PT, NW, KG>;
     constexpr int NQ = G::NQ;
     using Acc = typename std::conditional<PLANES, v4f, v4i>::type;
-    extern __shared__ __align__(16) unsigned char lds[];
-    const int tid = threadIdx.x;
+    extern __shared__ __align__(16) unsigned char all_lds[];
+    const int tid = threadIdx.x % G::NT;  // in the group
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / G::NT);
+    unsigned char *lds = all_lds + kg * G::GROUP;
     const int j = lane & 15, g = lane >> 4;
     const int lid = logical_block_id();
     const int mtiles = (a.m + G::TM - 1) / G::TM;
@@ -104,39 +109,43 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     const int whole = row_bytes >> 7;
     const int first = !PLANES && (row_bytes & 127) ? 1 : 0;
     const int steps = whole + first;
+    // the group's turn i is step KG*i + kg; every group makes the same number of turns (they share the barriers), the last of them with zeros
+    // where there is no step left
+    const int turns = (steps + KG - 1) / KG;
     constexpr int D = G::D;
-    v4i xring[D][NQ];  // step q in slot q % D
+    v4i xring[D][NQ];  // turn i in slot i % D
     // (what is asked for behind the last step repeats it, and a row without a whole step reads the row numbers: neither is used.  A
     // test around the loads would make the compiler wait for the newest instead of the one it needs)
-    auto load_x = [&](int q, v4i(&xr)[NQ]) __attribute__((always_inline)) {
-        const int at = 128 * max(min(q, steps - 1) - first, 0) + 16 * piece;
+    auto load_x = [&](int i_, v4i(&xr)[NQ]) __attribute__((always_inline)) {
+        const int at = 128 * max(min(KG * i_ + kg, steps - 1) - first, 0) + 16 * piece;
 #pragma unroll
         for (int i = 0; i < NQ; ++i) xr[i] = *reinterpret_cast<const v4i_u *>(src[i] + at);
     };
-    auto put_x = [&](int slab, const v4i(&xr)[NQ]) __attribute__((always_inline)) {
+    auto put_x = [&](int i_, int slab, const v4i(&xr)[NQ]) __attribute__((always_inline)) {
+        const bool none = KG > 1 && KG * i_ + kg >= steps;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) *reinterpret_cast<v4i *>(lds + slab * G::SLAB + (tid + G::NT * q) * 16) = xr[q];
+        for (int q = 0; q < NQ; ++q) *reinterpret_cast<v4i *>(lds + slab * G::SLAB + (tid + G::NT * q) * 16) = none ? v4i{0, 0, 0, 0} : xr[q];
     };
 
     // ---- codes: 16 words of each of the wavefront's 64 channels at a time, 4 word steps; instruction r of a load: channel
     // 16*r + (lane >> 2), word step lane & 3.  A word step is 64 channels of input; planes follow each other.  Words past a row's end are replaced
     // by its last one: they meet zeros of the other operand.
     constexpr int WS = PLANES ? 1 : 2;   // word steps of a step
-    constexpr int GS = 4 / WS;           // steps of a group of codes
+    constexpr int GS = 4 / WS;           // turns of a set of codes
     unsigned char *codes = lds + 2 * G::SLAB + wave * G::WAVE;
     const int wsteps = PLANES ? a.Kp >> 6 : 0x7fffffff;  // word steps of one plane
     const int wpiece = lane & 3;
     const uint32_t *wrow[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) wrow[r] = a.wq + (size_t)min(n0 + 16 * r + (lane >> 2), Nc - 1) * KW;
-    // groups requested ahead: with small tiles a group of int8 lasts two short steps, and codes come from memory as late as rows do
+    // sets of codes requested ahead: with small tiles one of int8 lasts two short steps, and codes come from memory as late as rows do
     constexpr int DW = D > 1 && !PLANES ? 2 : 1;
     struct Words {
         v4i v[4];
         int shift;  // words that lie before the ones wanted: a row's last ones are read as the row's last four
-    } wring[DW];    // group q in slot q % DW
-    auto load_w = [&](int group, Words &w) __attribute__((always_inline)) {
-        const int q = min(GS * group + wpiece / WS, steps - 1);
+    } wring[DW];    // set q in slot q % DW
+    auto load_w = [&](int set, Words &w) __attribute__((always_inline)) {
+        const int q = min(KG * (GS * set + wpiece / WS) + kg, steps - 1);
         int ws = WS * (q < first ? whole : q - first) + wpiece % WS;
         if constexpr (PLANES) {
             if (ws >= wsteps) ws -= wsteps;
@@ -168,9 +177,9 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[i][t] = Acc{0, 0, 0, 0};
 
-    int *lrow = reinterpret_cast<int *>(lds + G::ROWS);  // [TM] row, [TM] adapter (kNone: none), [TM] step
+    int *lrow = reinterpret_cast<int *>(all_lds + G::ROWS);  // [TM] row, [TM] adapter (kNone: none), [TM] step
     float *lstep = reinterpret_cast<float *>(lrow + 2 * G::TM);
-    float *lws = reinterpret_cast<float *>(lds + G::CHANS);  // [TN] w_scale, [TN] bias
+    float *lws = reinterpret_cast<float *>(all_lds + G::CHANS);  // [TN] w_scale, [TN] bias
     if (KW >= 4) load_w(0, wring[0]);
     else {  // one group holds every word of such a row; nothing behind it is used, and it is read from where there is something
 #pragma unroll
@@ -233,28 +242,31 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         load_low(adapter0, 0);
     };
     if constexpr (!EARLY) put_info();
-    if (first) {
+    if (first && kg == 0) {
         const int at = 128 * whole + 16 * piece;
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             Piece<int8_t, 16> v;
             v.load_some(reinterpret_cast<const int8_t *>(src[q] + at), row_bytes - at);
             xring[0][q] = __builtin_bit_cast(v4i, v);
-            if (whole == 0) src[q] = reinterpret_cast<const unsigned char *>(a.rows);
         }
-    } else
-        load_x(0, xring[0]);
+    }
+    if (whole == 0)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) src[q] = reinterpret_cast<const unsigned char *>(a.rows);
+    if (!(first && kg == 0)) load_x(0, xring[0]);
 #pragma unroll
     for (int d = 1; d < D; ++d) load_x(d, xring[d]);
     put_w(wring[0]);
     load_w(DW, wring[0]);
-    put_x(0, xring[0]);
+    put_x(0, 0, xring[0]);
     load_x(D, xring[0]);
-    if constexpr (EARLY) load_first();
+    if constexpr (EARLY)
+        if (kg == 0) load_first();
     lds_only_barrier();
 
     const int sw = (j & 7);
-    auto step = [&](auto turn, int s) __attribute__((always_inline)) {  // turn = s % 4
+    auto step = [&](auto turn, int s) __attribute__((always_inline)) {  // the group's turn s; turn = s % 4
         const int TURN = turn, NEXT = (TURN + 1) % D;
         const unsigned char *slab = lds + (TURN & 1) * G::SLAB + j * 128;
         uint32_t wc[WS][4];
@@ -262,7 +274,7 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
         for (int h = 0; h < WS; ++h)
 #pragma unroll
             for (int t = 0; t < 4; ++t) wc[h][t] = *reinterpret_cast<const uint32_t *>(wget + (WS * (TURN % GS) + h) * kCodeStep + 256 * t);
-        put_x((TURN + 1) & 1, xring[NEXT]);
+        put_x(s + 1, (TURN + 1) & 1, xring[NEXT]);
         load_x(s + 1 + D, xring[NEXT]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -292,18 +304,35 @@ __global__ __launch_bounds__(64 * NW, 2) void lora_gemm_kernel(const LoraGemmArg
     };
     static_assert(4 % D == 0 && 4 % GS == 0, "the turns below");
     int s = 0;
-    if constexpr (D == 1) {  // (the large tile's registers do not hold four steps' code: 142 us against 182)
-        for (; s < steps; ++s) step(s & 3, s);
+    if constexpr (D == 1) {  // (the large tile's registers do not hold four turns' code: 142 us against 182)
+        for (; s < turns; ++s) step(s & 3, s);
     } else {
-        for (; s + 4 <= steps; s += 4) {
+        for (; s + 4 <= turns; s += 4) {
             step(std::integral_constant<int, 0>{}, s);
             step(std::integral_constant<int, 1>{}, s + 1);
             step(std::integral_constant<int, 2>{}, s + 2);
             step(std::integral_constant<int, 3>{}, s + 3);
         }
-        if (s < steps) step(std::integral_constant<int, 0>{}, s);
-        if (s + 1 < steps) step(std::integral_constant<int, 1>{}, s + 1);
-        if (s + 2 < steps) step(std::integral_constant<int, 2>{}, s + 2);
+        if (s < turns) step(std::integral_constant<int, 0>{}, s);
+        if (s + 1 < turns) step(std::integral_constant<int, 1>{}, s + 1);
+        if (s + 2 < turns) step(std::integral_constant<int, 2>{}, s + 2);
+    }
+
+    if constexpr (KG > 1) {
+        if (kg > 0) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) *reinterpret_cast<Acc *>(lds + ((wave * PT + i) * 4 + t) * 1024 + lane * 16) = acc[i][t];
+        }
+        lds_only_barrier();
+        if (kg > 0) return;  // (a barrier waits for the wavefronts that are left)
+#pragma unroll
+        for (int o = 1; o < KG; ++o)
+#pragma unroll
+            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[i][t] += *reinterpret_cast<const Acc *>(all_lds + o * G::GROUP + ((wave * PT + i) * 4 + t) * 1024 + lane * 16);
     }
 
     // ---- epilogue: lane (j, g), register e of tile (i, t): row 16i + j, channel n0 + 16t + 4g + e --------------------
@@ -587,26 +616,30 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
 }
 
 // ---- launch ----------------------------------------------------------------------------------------------------
-template <int PT, int NW, bool PLANES, typename TO, typename TA> static void gemm_launch(const LoraGemmArgs &a, hipStream_t st)
+template <int PT, int NW, int KG, bool PLANES, typename TO, typename TA> static void gemm_launch(const LoraGemmArgs &a, hipStream_t st)
 {
-    using G = LoraGeom<PT, NW>;
+    using G = LoraGeom<PT, NW, KG>;
     const int ntiles = (a.Nc + G::TN - 1) / G::TN;
     const long long mtiles = (a.m + G::TM - 1) / G::TM;
-    hipLaunchKernelGGL((lora_gemm_kernel<PT, NW, PLANES, TO, TA>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(G::NT), G::LDS, st, a, ntiles);
+    static_assert(G::LDS <= 64 * 1024, "what a launch takes without asking");
+    hipLaunchKernelGGL((lora_gemm_kernel<PT, NW, KG, PLANES, TO, TA>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(G::NT * KG), G::LDS, st, a, ntiles);
 }
 
 template <bool PLANES, typename TO, typename TA> static void gemm_pick(const LoraGemmArgs &a, hipStream_t st)
 {
-    // The largest tile that still gives every compute unit a workgroup (the largest of all two: it runs two at a time), measured
-    // (us, tiles 128x256 / 64x256 / 32x256 / 32x128, int8): 8192 x 4096 x 4096 118 / 133 / 165 / 193, 2048 x 4096 x 4096 47 / 39 / 51 / 61,
-    // 512 x 4096 x 4096 39 / 26 / 22 / 25, 128 x 4096 x 4096 45 / 28 / 21 / 20; up to 128 channels half of a wide tile is empty
-    // (12544 x 512 x 128: 16 / 11 / 11 / 10).
+    // The largest tile that still gives every compute unit a workgroup (the largest of all two: it runs two at a time), and with few small
+    // tiles two groups of wavefronts that halve the chain of steps.  Measured (us, tiles 128x256 / 64x256 / 32x256 / 32x128 / 32x128 by two
+    // groups, int8): 8192 x 4096 x 4096 118 / 130 / 186 / 191 / 232, 2048 x 4096 x 4096 47 / 39 / 52 / 53 / 64,
+    // 512 x 4096 x 4096 39 / 25 / 21 / 24 / 20, 128 x 4096 x 4096 45 / 27 / 21 / 18 / 14, 12544 x 960 x 160 23 / 16 / 15 / 15 / 22; three planes of
+    // 1671 x 2474 x 457 - / 72 / 56 / 51 / 34 (by three groups 32); 100 x 500 x 600, 8 steps, - / 14 / 12 / 12 / 10.
     auto tiles = [&](int tm, int tn) { return (long long)((a.m + tm - 1) / tm) * ((a.Nc + tn - 1) / tn); };
-    if (a.Nc <= 128) gemm_launch<2, 2, PLANES, TO, TA>(a, st);
-    else if (tiles(128, 256) >= 512) gemm_launch<8, 4, PLANES, TO, TA>(a, st);
-    else if (tiles(64, 256) >= 256) gemm_launch<4, 4, PLANES, TO, TA>(a, st);
-    else if (tiles(32, 256) >= 256) gemm_launch<2, 4, PLANES, TO, TA>(a, st);
-    else gemm_launch<2, 2, PLANES, TO, TA>(a, st);
+    const int steps = PLANES ? a.planes * a.Kp / 64 : (a.K + 127) / 128;
+    if (tiles(32, 128) <= 512 && steps >= 8) gemm_launch<2, 2, 2, PLANES, TO, TA>(a, st);
+    else if (a.Nc <= 128) gemm_launch<2, 2, 1, PLANES, TO, TA>(a, st);  // half of a wider tile would be empty
+    else if (tiles(128, 256) >= 512) gemm_launch<8, 4, 1, PLANES, TO, TA>(a, st);
+    else if (tiles(64, 256) >= 256) gemm_launch<4, 4, 1, PLANES, TO, TA>(a, st);
+    else if (tiles(32, 256) >= 256) gemm_launch<2, 4, 1, PLANES, TO, TA>(a, st);
+    else gemm_launch<2, 2, 1, PLANES, TO, TA>(a, st);
 }
 
 template <typename F> static void by_types(int adapter_type, int out_type, F f)

@@ -513,7 +513,7 @@ typedef struct {
  *             can overlap in time need one each.  has_hid: whether hid is given; up to 64 rows need no workspace then (0 bytes, as for
  *             sizes that the call refuses).
  * Any channels, rows, rank and alignment to elements (w_packed: 4 bytes).  PROM_EINVAL for null or misaligned pointers,
- * non-positive sizes, other types; PROM_EUNSUPPORTED above 65536 channels, rank 128, 65535 adapters or 2^30 - 1 rows; PROM_EALIAS if an
+ * non-positive sizes, other types; PROM_EUNSUPPORTED above 65536 channels, rank 128, 65535 adapters or 2^26 rows; PROM_EALIAS if an
  * output overlaps an input or another output; PROM_EWORKSPACE. */
 int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, const void *w_packed, int cout, const float *x_step,
                       const float *w_scale, const float *bias, const prom_lora_t *lora, void *y, int y_type, float *hid,
@@ -616,7 +616,7 @@ typedef struct {
  * caller (8-byte aligned) and passed to every step with the plan.  It holds the tensors' addresses: build it anew when one moves.
  * Tensors may lie anywhere, aligned to their elements; an output that overlaps its tensor's gradient or another of its outputs is
  * PROM_EALIAS (tensors are not compared with each other: they must not overlap).  PROM_EINVAL for null or misaligned pointers,
- * n <= 0, an unknown type or state_bits; the offending tensor's index goes to *bad_tensor if not NULL.  0 bytes where prom_adamw_table would fail. */
+ * n <= 0, an unknown type or state_bits, PROM_EUNSUPPORTED above 2^24 - 1 workgroups of 4096 elements; the offending tensor's index goes to *bad_tensor if not NULL.  0 bytes where prom_adamw_table would fail. */
 size_t prom_adamw_table_size(const prom_adamw_tensor_t *tensors, int count);
 int prom_adamw_table(const prom_adamw_tensor_t *tensors, int count, void *table_host, size_t table_bytes,
                      prom_adamw_plan_t *plan, int *bad_tensor);

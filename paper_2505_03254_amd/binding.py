@@ -667,6 +667,14 @@ def _launch(fn, where, dev, stream, *args):
         raise PromError(rc, where)
 
 
+def _lend(stream, *tensors):
+    """Tensors that a call allocated are used on `stream`: their memory is not handed out again before that work is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _norm_rows(x):
     cols = x.shape[-1] if x.dim() else 0
     if not cols or not x.numel():
@@ -687,6 +695,7 @@ def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=No
     _launch((_lib or load_library()).prom_layernorm, "prom_layernorm", dev, stream, px, _type_of(x.dtype), rows, cols,
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
             _ptr(y, "y", x.dtype, x.shape, dev), _ptr(mean, "mean", f32, by_row, dev), _ptr(rstd, "rstd", f32, by_row, dev))
+    _lend(stream, y, mean, rstd)
     return y, mean, rstd
 
 
@@ -706,6 +715,7 @@ def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
             quant_eps, _ptr(q, "q", torch.int8, x.shape, dev), _ptr(step, "step", f32, by_row, dev), _ptr(mean, "mean", f32, by_row, dev),
             _ptr(rstd, "rstd", f32, by_row, dev))
+    _lend(stream, q, step, mean, rstd)
     return q, step, mean, rstd
 
 
@@ -735,6 +745,7 @@ def prom_layernorm_backward(dy, x, weight, mean, rstd, want_dx: bool = True, wan
             _ptr(rstd, "rstd", f32, by_row, dev), dx.data_ptr() if want_dx else None, dweight.data_ptr() if want_dweight else None,
             dbias.data_ptr() if want_dbias else None, None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
             0 if workspace is None else workspace.numel() * workspace.element_size())
+    _lend(stream, dx, dweight, dbias, workspace)
     return dx, dweight, dbias
 
 
@@ -796,6 +807,7 @@ def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora,
             None if bias is None else _ptr(bias, "bias", f32, (cout,), dev), lc, py, _type_of(y.dtype), phid,
             None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
             0 if workspace is None else workspace.numel() * workspace.element_size())
+    _lend(stream, y, hid, workspace)
     return (y, hid) if want_hid else y
 
 
@@ -829,6 +841,7 @@ def prom_pw_conv_lora_backward(dy, x, x_step, wt_packed, w_scale, lora: Lora, hi
             None if hid is None else _ptr(hid, "hid", f32, (n * h * w, lc.rank), dev), dx.data_ptr() if want_dx else None,
             da.data_ptr() if want_da else None, db.data_ptr() if want_db else None, _ptr(workspace, "workspace", None, None, dev),
             workspace.numel() * workspace.element_size())
+    _lend(stream, dx, da, db, workspace)
     return dx, da, db
 
 

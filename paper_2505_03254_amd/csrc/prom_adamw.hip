@@ -319,7 +319,7 @@ static int adam_check(const prom_adamw_tensor_t *t, int count, int *bad)
         if (outputs_meet(out, 6, in, 1)) return PROM_EALIAS;
     }
     if (bad) *bad = -1;
-    if (adam_chunks(t, count) > 0x7fffffffLL) return PROM_EUNSUPPORTED;
+    if (adam_chunks(t, count) > 0xffffffLL) return PROM_EUNSUPPORTED;  // a launch has fewer than 2^32 threads
     return PROM_OK;
 }
 

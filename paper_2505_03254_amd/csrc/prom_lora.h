@@ -22,8 +22,9 @@ typedef int v4i_u __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraMaxChannels = 65536;  // |64 * acc| < 2^31 and |acc| < 2^24 exact in float32
 constexpr int kLoraMaxAdapters = 65535;
+constexpr long long kLoraMaxRows = 1LL << 26;  // a launch has fewer than 2^32 threads: 512 for 16 rows
 
-// Planes of a type; of two planes' product only those that reach 2^-24 of the whole are taken (see plane_pairs).
+// Planes of a type; of the products of two split numbers those are taken that reach 2^-24 of the whole.
 template <typename T> constexpr int planes_of() { return sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2; }
 
 template <int P> __device__ __forceinline__ void split(float v, bf16_t (&out)[P])
@@ -75,7 +76,7 @@ struct LoraPlan {
 struct LoraGemmArgs {
     const void *x;       // int8 [m][K], or bf16 planes [m][planes][Kp]
     const uint32_t *wq;  // packed [Nc][KW]
-    const int *rows;     // row numbers by position, NULL: position = row
+    const int *rows;     // row numbers by position (not looked at for a few rows)
     const int *index;    // adapter by batch element
     const float *step, *w_scale, *bias;  // (int8 input)
     const float *hid;    // [m][rank] scaled by the adapter's scale here (scale != NULL) or already

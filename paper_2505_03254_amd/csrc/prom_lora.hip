@@ -550,7 +550,7 @@ static int lora_check(int n, int h, int w, int cin, int cout, const void *wq, co
     if (misaligned(wq, 4) || misaligned(lo->a, 2) || misaligned(lo->b, 2) || misaligned(lo->scale, 4) || misaligned(lo->index, 4)) return PROM_EINVAL;
     if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || lo->rank > kLoraMaxRank || lo->adapters > kLoraMaxAdapters) return PROM_EUNSUPPORTED;
     const long long hw = (long long)h * w;
-    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return PROM_EUNSUPPORTED;
+    if (hw > kLoraMaxRows || hw * n > kLoraMaxRows) return PROM_EUNSUPPORTED;
     *m = hw * n;
     return PROM_OK;
 }
@@ -568,7 +568,7 @@ static bool lora_sizes(int n, int h, int w, int cin, int cout, int adapters, int
     if (n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0 || adapters <= 0 || rank <= 0) return false;
     if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || rank > kLoraMaxRank || adapters > kLoraMaxAdapters) return false;
     const long long hw = (long long)h * w;
-    if (hw > 0x3fffffffLL || hw * n > 0x3fffffffLL) return false;
+    if (hw > kLoraMaxRows || hw * n > kLoraMaxRows) return false;
     *m = hw * n;
     return true;
 }

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void norm_kernel(const NormArgs 
     const int lane = threadIdx.x & 63;
     const int wave = threadIdx.x >> 6;
     const int wv = wave % WPR, slot = wave / WPR;
-    const long long mine = (long long)blockIdx.x * G::ROWS + slot;
+    const long long mine = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * G::ROWS + slot;
     const bool live = mine < a.rows;
     const long long row = live ? mine : a.rows - 1;  // a wavefront without a row repeats the last one and writes nothing
     const int C = a.cols;
@@ -381,7 +381,9 @@ static int norm_nv(int cols, int wpr, int bytes)
 template <typename T, int NV, int WPR> static void norm_launch(const NormArgs &a, bool quant, hipStream_t st)
 {
     using G = NormGeom<T, NV, WPR>;
-    const dim3 grid((unsigned)((a.rows + G::ROWS - 1) / G::ROWS)), block(64 * G::WAVES);
+    // (a dimension of a launch has fewer than 2^32 threads)
+    const long long groups = (a.rows + G::ROWS - 1) / G::ROWS, most = 1LL << 20;
+    const dim3 grid((unsigned)(groups < most ? groups : most), (unsigned)((groups + most - 1) / most)), block(64 * G::WAVES);
     if (quant) hipLaunchKernelGGL((norm_kernel<T, NV, WPR, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((norm_kernel<T, NV, WPR, false>), grid, block, 0, st, a);
 }

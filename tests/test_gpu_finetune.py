@@ -149,3 +149,28 @@ def test_two_calls_at_once_on_two_streams(P):
     for m, r in zip(got, ref):
         for k in m.params:
             assert torch.equal(m.params[k], r.params[k]), k
+
+
+def test_a_stream_given_to_the_calls(P):
+    """stream=: work enqueued behind it on the current stream does not get the call's workspace while it runs."""
+    m = Model(P, 32)
+    torch = m.torch
+    q, step, mean, rstd = P.prom_layernorm_quant(m.x, m.params["weight"], m.params["bias"])
+    lora = P.Lora(m.copies["a"], m.copies["b"], m.scale, m.index)
+    x4 = q.view(ROWS, 1, 1, CIN)
+    y, hid = P.prom_pw_conv_lora(x4, m.packed, COUT, step, m.w_scale, None, lora, want_hid=True)
+    dy = m.target.view(ROWS, 1, 1, COUT)
+    want = P.prom_pw_conv_lora_backward(dy, x4, step, m.packed_t, m.w_scale, lora, hid)
+    wn = P.prom_layernorm_backward(want[0].view(ROWS, CIN), m.x, m.params["weight"], mean, rstd)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        got = P.prom_pw_conv_lora_backward(dy, x4, step, m.packed_t, m.w_scale, lora, hid, stream=side)
+        gn = P.prom_layernorm_backward(got[0].view(ROWS, CIN), m.x, m.params["weight"], mean, rstd, stream=side)
+        gy, gh = P.prom_pw_conv_lora(x4, m.packed, COUT, step, m.w_scale, None, lora, want_hid=True, stream=side)
+        gq = P.prom_layernorm_quant(m.x, m.params["weight"], m.params["bias"], stream=side)
+        for size in (1 << 14, 1 << 18, 1 << 20, 1 << 21):
+            torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        for u, v in zip(got + gn + (gy, gh) + gq, want + wn + (y, hid) + (q, step, mean, rstd)):
+            assert torch.equal(u, v)

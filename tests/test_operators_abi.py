@@ -39,7 +39,7 @@ def backward(lib, lo=None, **k):
 @pytest.mark.parametrize("k,code", [
     (dict(x=None), -1), (dict(wp=None), -1), (dict(step=None), -1), (dict(ws=None), -1), (dict(y=None), -1), (dict(n=0), -1), (dict(h=-1), -1),
     (dict(cin=0), -1), (dict(cout=-3), -1), (dict(yt=2), -1), (dict(yt=3), -1), (dict(wp=W + 2), -1), (dict(y=Y + 1), -1), (dict(yt=0, y=Y + 2), -1),
-    (dict(hid=H + 2), -1), (dict(bias=S + 2), -1), (dict(cin=65537), -2), (dict(cout=65537), -2), (dict(n=1 << 30), -2), (dict(n=1 << 16, h=1 << 10, w=1 << 10), -2),
+    (dict(hid=H + 2), -1), (dict(bias=S + 2), -1), (dict(cin=65537), -2), (dict(cout=65537), -2), (dict(n=1 << 30), -2), (dict(n=(1 << 26) + 1), -2), (dict(n=1 << 16, h=1 << 10, w=1 << 10), -2),
     (dict(space=None), -4), (dict(bytes=100), -4), (dict(space=WS + 8), -4), (dict(y=X + 10), -3), (dict(y=A + 2), -3), (dict(hid=Y + 64), -3), (dict(y=WS), -3),
     (dict(hid=I), -3), (dict(n=64, hid=None, space=None), -4)])
 def test_forward_refuses(lib, k, code):

@@ -17,10 +17,14 @@ _torch = None  # torch, from the first call that needs it on (importing this pac
 PROM_OK = 0
 
 
+_raw_stream = _get_device = None  # two of its functions that every launch asks
+
+
 def _import_torch():
-    global _torch
+    global _torch, _raw_stream, _get_device
     import torch
     _torch = torch
+    _raw_stream, _get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     return torch
 
 
@@ -652,17 +656,16 @@ def _input(t, name):
 
 def _launch(fn, where, dev, stream, *args):
     """fn(*args, stream) with the tensors' device current, on its current stream or on `stream`."""
-    torch = _torch
-    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
-    back = torch._C._cuda_getDevice()
+    s = _raw_stream(dev) if stream is None else int(stream.cuda_stream)
+    back = _get_device()
     if back == dev:
         rc = fn(*args, s)
     else:
-        torch.cuda.set_device(dev)
+        _torch.cuda.set_device(dev)
         try:
             rc = fn(*args, s)
         finally:
-            torch.cuda.set_device(back)
+            _torch.cuda.set_device(back)
     if rc:
         raise PromError(rc, where)
 
@@ -673,6 +676,14 @@ def _lend(stream, *tensors):
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
+
+
+def _out(t, name, like, dtype, shape, dev):
+    """An output and its address: the caller's, checked, or a new one (quickest where it is like another tensor)."""
+    if t is not None:
+        return t, _ptr(t, name, dtype, shape, dev)
+    t = _torch.empty_like(like) if like.dtype is dtype and like.shape == shape else _torch.empty(shape, dtype=dtype, device=like.device)
+    return t, t.data_ptr()
 
 
 def _norm_rows(x):
@@ -689,12 +700,12 @@ def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=No
     px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
     f32, by_row, by_col = torch.float32, (rows,), (cols,)
-    y = torch.empty_like(x) if y is None else y
-    mean = torch.empty(rows, dtype=f32, device=x.device) if mean is None else mean
-    rstd = torch.empty_like(mean) if rstd is None else rstd
+    y, py = _out(y, "y", x, x.dtype, x.shape, dev)
+    mean, pm = _out(mean, "mean", x, f32, by_row, dev)
+    rstd, pr = _out(rstd, "rstd", mean, f32, by_row, dev)
     _launch((_lib or load_library()).prom_layernorm, "prom_layernorm", dev, stream, px, _type_of(x.dtype), rows, cols,
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
-            _ptr(y, "y", x.dtype, x.shape, dev), _ptr(mean, "mean", f32, by_row, dev), _ptr(rstd, "rstd", f32, by_row, dev))
+            py, pm, pr)
     _lend(stream, y, mean, rstd)
     return y, mean, rstd
 
@@ -707,14 +718,13 @@ def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps
     px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
     f32, by_row, by_col = torch.float32, (rows,), (cols,)
-    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if q is None else q
-    step = torch.empty(rows, dtype=f32, device=x.device) if step is None else step
-    mean = torch.empty_like(step) if mean is None else mean
-    rstd = torch.empty_like(step) if rstd is None else rstd
+    q, pq = _out(q, "q", x, torch.int8, x.shape, dev)
+    step, ps = _out(step, "step", x, f32, by_row, dev)
+    mean, pm = _out(mean, "mean", step, f32, by_row, dev)
+    rstd, pr = _out(rstd, "rstd", step, f32, by_row, dev)
     _launch((_lib or load_library()).prom_layernorm_quant, "prom_layernorm_quant", dev, stream, px, _type_of(x.dtype), rows, cols,
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
-            quant_eps, _ptr(q, "q", torch.int8, x.shape, dev), _ptr(step, "step", f32, by_row, dev), _ptr(mean, "mean", f32, by_row, dev),
-            _ptr(rstd, "rstd", f32, by_row, dev))
+            quant_eps, pq, ps, pm, pr)
     _lend(stream, q, step, mean, rstd)
     return q, step, mean, rstd
 

@@ -82,6 +82,8 @@ struct LoraGemmArgs {
     const float *hid;    // [m][rank] scaled by the adapter's scale here (scale != NULL) or already
     const float *scale;
     const void *low;     // [adapters][rank][Nc]
+    const void *first;   // [adapters][rank][K] (a few rows that form hid themselves)
+    float *hid_out;
     void *y;
     int m, hw, K, KW, Nc, rank, adapters, planes, Kp;
 };

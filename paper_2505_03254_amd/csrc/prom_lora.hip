@@ -626,7 +626,10 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     ga.adapters = lora->adapters;
     clear_hip_error();
     if (m <= kLoraFew) {
-        by_adapter_type(lora->type, [&](auto t) {
+        if (m * lora->rank <= kFuseMost) {
+            ga.first = lora->a;
+            ga.hid_out = hid;
+        } else by_adapter_type(lora->type, [&](auto t) {
             using T = decltype(t);
             auto go = [&](auto rc) {
                 constexpr int RC = decltype(rc)::value;

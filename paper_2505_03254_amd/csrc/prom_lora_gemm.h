@@ -9,7 +9,9 @@ inline int lora_padded(int channels) { return (channels + 63) / 64 * 64; }
 
 // Sorted rows (a.rows).  planes: the input is bf16 planes [m positions][a.planes][a.Kp] instead of int8 [m][K].
 void lora_gemm(const LoraGemmArgs &a, int adapter_type, int out_type, bool planes, hipStream_t st);
-// At most 64 rows in their own order, int8 input.
+// rows * rank up to which a few rows' product forms hid itself: a row's adapter passes every workgroup.
+constexpr int kFuseMost = 32;
+// At most 64 rows in their own order, int8 input.  With a.hid_out (at most kFuseMost numbers) hid is formed on the way from a.first and written there.
 void lora_gemm_few(const LoraGemmArgs &a, int adapter_type, int out_type, hipStream_t st);
 
 }  // namespace prom

@@ -488,10 +488,13 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
 // Four lanes read 64 bytes of a row (and 16 of a channel's codes) in one instruction: every row passes the texture addresser
 // in whole runs.  The low-rank term is one dot product over the ranks per output on the vector ALU, every row with its own adapter; its
 // operands are requested before the product, which they do not depend on.  Bound by latency, then by the adapters' bytes.
-template <typename TO, typename TA, int MT>
+// FUSE: for a token or two every workgroup forms hid itself (rank * cin * 2 bytes a row out of L2, 131 KB at 4096 channels and rank 16, while
+// the product's own loads are on their way) and no launch goes before this one.
+template <typename TO, typename TA, int MT, bool FUSE>
 __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a)
 {
     __shared__ v4i red[8][MT][64];
+    __shared__ float formed[FUSE ? kFuseMost : 1];
     constexpr int RP = 16;  // ranks requested ahead
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -559,7 +562,45 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
             for (int r = 0; r < RP; ++r) {
                 const int rr = min(r, a.rank - 1);
                 b[r].load_some(low + (size_t)rr * a.Nc, channels);
-                h[r] = hid[rr];
+                if constexpr (!FUSE) h[r] = hid[rr];
+            }
+        }
+        if constexpr (FUSE) {
+            for (int p = wave; p < a.m * a.rank; p += 8) {  // a wavefront per row and rank
+                const int prow = p / a.rank, r = p - prow * a.rank;
+                const int pel = a.hw == 1 ? prow : prow / a.hw;
+                const int pl = a.index[pel];
+                float s = 0.0f;
+                if (pl >= 0 && pl < a.adapters) {
+                    const int8_t *x = static_cast<const int8_t *>(a.x) + (size_t)prow * K;
+                    const TA *w = static_cast<const TA *>(a.first) + ((size_t)pl * a.rank + r) * K;
+                    auto dot = [&](auto whole, int k, int u) __attribute__((always_inline)) {
+                        constexpr bool WHOLE = decltype(whole)::value;
+                        constexpr int N = WHOLE ? 8 : 1;
+                        Piece<int8_t, 8> xv[N];
+                        Piece<TA, 8> wv[N];
+#pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            const int k0 = k + 512 * (n < u ? n : 0) + 8 * lane;
+                            xv[n].load_some(x + k0, WHOLE ? 8 : K - k0);
+                            wv[n].load_some(w + k0, WHOLE ? 8 : K - k0);
+                        }
+#pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            if (n >= u) break;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) s += (float)xv[n].e[e] * (float)wv[n].e[e];
+                        }
+                    };
+                    const int kw = K & ~511;
+                    for (int k = 0; k < kw; k += 4096) dot(std::true_type{}, k, min(8, (kw - k) >> 9));
+                    if (kw < K) dot(std::false_type{}, kw, 1);
+                    s = wave_sum_f32(s) * a.step[pel];
+                }
+                if (lane == 0) {
+                    formed[p] = s;
+                    if (n0 == 0) a.hid_out[p] = s;
+                }
             }
         }
     };
@@ -593,8 +634,10 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     float z0 = base_value(s0, ws.e[0], st, bi.e[0]), z1 = base_value(s1, ws.e[1], st, bi.e[1]);
     if (has) {
         float l0 = 0.0f, l1 = 0.0f;
+        if constexpr (FUSE) hid = formed + row * a.rank;
 #pragma unroll
         for (int r = 0; r < RP; ++r) {
+            if constexpr (FUSE) h[r] = hid[min(r, a.rank - 1)];
             const float v = r < a.rank ? h[r] : 0.0f;
             l0 += r < a.rank ? v * (float)b[r].e[0] : 0.0f;
             l1 += r < a.rank ? v * (float)b[r].e[1] : 0.0f;
@@ -667,9 +710,10 @@ void lora_gemm_few(const LoraGemmArgs &a, int adapter_type, int out_type, hipStr
         using TO = decltype(to);
         using TA = decltype(ta);
         const dim3 grid((unsigned)(((a.Nc + 15) / 16 + 7) / 8 * 8)), block(512);
-        if (a.m <= 16) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1>), grid, block, 0, st, a);
-        else if (a.m <= 32) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 2>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 4>), grid, block, 0, st, a);
+        if (a.hid_out) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1, true>), grid, block, 0, st, a);
+        else if (a.m <= 16) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1, false>), grid, block, 0, st, a);
+        else if (a.m <= 32) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 2, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 4, false>), grid, block, 0, st, a);
     });
 }
 

@@ -94,9 +94,10 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
     const int m0 = mtile * G::TM;
     const int K = a.K, KW = a.KW, Nc = a.Nc;
 
-    // ---- rows: piece idx = tid + NT*q of a slab is slot idx & 7 of row idx >> 3 and holds the row's piece slot ^ (row & 7)
+    // ---- rows: piece idx = tid + NT*q of a slab is slot idx & 7 of row idx >> 3 and holds the row's piece slot ^ ((row >> 1) & 7): two rows
+    // fill LDS's 64 banks, so that 16 rows' operands lie in different ones
     const int row_bytes = PLANES ? a.planes * a.Kp * 2 : K;
-    const int piece = (tid & 7) ^ ((tid >> 3) & 7);
+    const int piece = (tid & 7) ^ ((tid >> 4) & 7);
     const unsigned char *src[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
         if (kg == 0) load_first();
     lds_only_barrier();
 
-    const int sw = (j & 7);
+    const int sw = (j >> 1) & 7;
     auto step = [&](auto turn, int s) __attribute__((always_inline)) {  // the group's turn s; turn = s % 4
         const int TURN = turn, NEXT = (TURN + 1) % D;
         const unsigned char *slab = lds + (TURN & 1) * G::SLAB + j * 128;

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * kNormGradWaves) void norm_grad_kernel(const No
     constexpr int VE = 16 / sizeof(T);
     constexpr int ROWS = kNormGradWaves / WPR;
     __shared__ float part[2][2][kNormGradWaves];
-    extern __shared__ float sums[];  // [2][cols] when ROWS > 1
+    extern __shared__ float sums[];  // [2][columns of a row's registers] when ROWS > 1
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wv = wave % WPR, slot = wave / WPR;
@@ -302,19 +302,18 @@ __global__ __launch_bounds__(64 * kNormGradWaves) void norm_grad_kernel(const No
             for (int i = 0; i < NV; ++i) {
                 const int c0 = ((i * WPR + wv) * 64 + lane) * VE;
                 Piece<float, VE> w, b;
-                if (k) {
-                    w.load_some(sums + c0, C - c0);
-                    b.load_some(sums + C + c0, C - c0);
-                }
+                float *s = sums + (i * VE * WPR + wv) * 64 + lane;  // element e: 64 * WPR further each, one bank per lane
+                constexpr int B = NV * VE * WPR * 64;
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    w.e[e] = k ? w.e[e] + dw[i][e] : dw[i][e];
-                    b.e[e] = k ? b.e[e] + db[i][e] : db[i][e];
+                    w.e[e] = k ? s[e * WPR * 64] + dw[i][e] : dw[i][e];
+                    b.e[e] = k ? s[e * WPR * 64 + B] + db[i][e] : db[i][e];
+                    if (k < ROWS - 1) {
+                        s[e * WPR * 64] = w.e[e];
+                        s[e * WPR * 64 + B] = b.e[e];
+                    }
                 }
-                if (k < ROWS - 1) {
-                    w.store_some(sums + c0, C - c0);
-                    b.store_some(sums + C + c0, C - c0);
-                } else {
+                if (k == ROWS - 1) {
                     w.store_some(out + c0, C - c0);
                     b.store_some(out + C + c0, C - c0);
                 }
@@ -390,7 +389,7 @@ template <typename T, int NV, int WPR> static void norm_launch(const NormArgs &a
 template <typename T, int NV, int WPR> static void norm_grad_launch(const NormGradArgs &a, int parts, hipStream_t st)
 {
     hipLaunchKernelGGL((norm_grad_kernel<T, NV, WPR>), dim3((unsigned)parts), dim3(64 * kNormGradWaves),
-                       WPR < kNormGradWaves && a.want ? (size_t)8 * a.cols : 0, st, a);
+                       WPR < kNormGradWaves && a.want ? (size_t)8 * 64 * WPR * NV * (16 / sizeof(T)) : 0, st, a);
 }
 // f(NV, WPR) as integral constants
 template <typename F> static void norm_pick(int nv, int wpr, F f)

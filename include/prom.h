@@ -10,6 +10,9 @@
  *   - the int8 depthwise 3x3 convolution that sits between two pointwise convolutions
  *     (Section 2, first paragraph; Section 3.1 "Depthwise Convolutions", Eq. 4-5);
  *   - the block expand -> depthwise -> project with optional skip (Section 2; Figure 4).
+ * Beside them stand, for models whose ternary weights stay fixed while something small is learned on top: the pointwise layer
+ * with the low-rank adapters of many requests (prom_pw_conv_lora) and its gradients, the layer norm that feeds it (prom_layernorm)
+ * and the AdamW step that trains both (prom_adamw_step).
  *
  * Conventions shared by every entry point
  *   Layout      activations are int8 NHWC, dense (no strides); a pointwise layer sees them
@@ -492,7 +495,8 @@ enum { PROM_F32 = 0, PROM_BF16 = 1, PROM_F16 = 2 };
  *   y[m][co]  = (acc[m][co] * w_scale[co]) * x_step[i] + bias[co] + scale[l] * sum_r hid[m][r] * b[l][r][co]
  * acc the int32 accumulator of prom_pw_conv, everything real in float32 (up to the bias three operations, each rounded once,
  * as in prom_pw_conv_dynq), one rounding to y's type at the end.
- * An index outside [0, adapters) means no adapter: the sum over r is left out and hid is zero.  Nothing an adapter
+ * An index outside [0, adapters) means no adapter: the sum over r is left out and hid is zero.  (More than 64 rows are sorted by adapter
+ * first, which reads `index` once per adapter; batch elements may come in any order.)  Nothing an adapter
  * holds (infinities, NaN) reaches rows that do not take it.
  *   a      dev [adapters][rank][cin] of `type` (PROM_BF16 or PROM_F16)
  *   b      dev [adapters][rank][cout] of `type`: row r is the r-th direction in the output channels

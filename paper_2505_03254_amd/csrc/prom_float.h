@@ -17,7 +17,7 @@ typedef _Float16 f16_t;
 inline int type_bytes(int type) { return type == PROM_F32 ? 4 : type == PROM_BF16 || type == PROM_F16 ? 2 : 0; }
 
 // A pointer known to point to global memory.  One that comes out of memory may point anywhere to the compiler, and its flat accesses
-// wait for LDS as well as for each other (AdamW, whose pointers stand in a table: 257 us with flat accesses, see adamw_kernel for without).
+// wait for LDS as well as for each other (AdamW, whose pointers stand in a table, 75 M elements in 8 bits: 257 us flat, 252 global).
 template <typename T> using Global = T __attribute__((address_space(1)));
 
 // A piece of 16 (8, 4) bytes at an address that is aligned to its elements only: gfx950 loads and stores dwords at any

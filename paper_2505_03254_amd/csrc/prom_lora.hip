@@ -62,10 +62,20 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (b[e] >> lane & 1) p.order[mine++] = i + 4 * lane + e;
+            if (b[e] >> lane & 1) {
+                if (hw == 1) p.rows[mine] = i + 4 * lane + e;
+                p.order[mine++] = i + 4 * lane + e;
+            }
         at += all;
     }
     const int first = lower * hw, count = total * hw;
+    if (hw > 1) {
+        __syncthreads();  // (the elements above are this workgroup's own: visible to all of it behind the barrier)
+        for (int i = threadIdx.x; i < count; i += 1024) {
+            const int e = i / hw;
+            p.rows[first + i] = p.order[lower + e] * hw + (i - e * hw);
+        }
+    }
     if (threadIdx.x == 0) p.groups[l] = int2{first, count};
     auto cut = [&](int4 *out, int tile) {
         const int base = first / tile + l, end = (first + count) / tile + l + 1;
@@ -84,14 +94,13 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
 struct LoraShrinkArgs {
     const void *in;     // int8 x [m][K] or dy [m][K]
     const void *low;    // [adapters][rank][K]
-    const int *order;
+    const int *rows;    // [m] in sorted order
     const int4 *tiles;
     const float *step;  // [n]
     const float *scale; // [adapters] (backward)
     const float *w_scale;
     float *out;         // [m][rank]
     float *out_step;    // backward: out * step [m][rank]
-    int *rows;          // [m], written
     bf16_t *planes;     // backward: [m positions][P][Kp] or NULL
     int hw, K, Kp, rank, adapters;
 };
@@ -127,11 +136,8 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         in[i] = 16 * i + j < count;
-        const int pos = tile.y + min(16 * i + j, count - 1);
-        const int e = pos / a.hw;
-        elem[i] = a.order[e];
-        row[i] = elem[i] * a.hw + (pos - e * a.hw);
-        if (wave == 0 && g == 0 && in[i]) a.rows[pos] = row[i];
+        row[i] = a.rows[tile.y + min(16 * i + j, count - 1)];
+        elem[i] = a.hw == 1 ? row[i] : row[i] / a.hw;
     }
     v4f acc[I][RT];
 #pragma unroll
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     }
 }
 
-// The same for a few rows, without sorting: a wavefront per row and RC ranks, the channels over its lanes, float32 on the vector
+// The same for fewer rows, without sorting: a wavefront per row and RC ranks, the channels over its lanes, float32 on the vector
 // ALU.  Every row reads its own adapter; what bounds it is the latency of two dependent loads and, with many rows, the adapters' bytes (64 rows of
 // 4096 channels, rank 16, 64 adapters: 4.0 us).
 template <typename TA, int RC>
@@ -562,6 +568,10 @@ static int lora_check(int n, int h, int w, int cin, int cout, const void *wq, co
 // Up to this many rows run without sorting, on the kernels whose workgroups hold every row.
 constexpr int kLoraFew = 64;
 
+// rows * rank up to which the shrinking product of the forward call goes row by row: the tiles of sorted rows are too few to fill the chip, and the
+// adapters, read once per row, still come out of L2 fast enough (4096 channels, 512 rows of rank 16 and 1000 of rank 8: 7.0 and 6.2 us, in tiles 16).
+constexpr int kLoraUnsorted = 16384;
+
 static int planes_of_type(int type) { return type == PROM_F32 ? 3 : type == PROM_F16 ? 2 : 1; }
 
 }  // namespace prom
@@ -629,11 +639,9 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     ga.rank = lora->rank;
     ga.adapters = lora->adapters;
     clear_hip_error();
-    if (m <= kLoraFew) {
-        if (m * lora->rank <= kFuseMost) {
-            ga.first = lora->a;
-            ga.hid_out = hid;
-        } else by_adapter_type(lora->type, [&](auto t) {
+    // Every row with its own adapter, without sorting: a rank per wavefront while that leaves SIMDs idle, four (which share the row's codes) from then on.
+    auto shrink_small = [&]() {
+        by_adapter_type(lora->type, [&](auto t) {
             using T = decltype(t);
             auto go = [&](auto rc) {
                 constexpr int RC = decltype(rc)::value;
@@ -641,10 +649,16 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
                 hipLaunchKernelGGL((lora_shrink_small_kernel<T, RC>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, x, static_cast<const T *>(lora->a),
                                    lora->index, x_step, hid, (int)m, ga.hw, cin, lora->rank, lora->adapters);
             };
-            // a rank per wavefront while that leaves SIMDs idle, four (which share the row's codes) from then on
             if (m * lora->rank <= 1024) go(std::integral_constant<int, 1>{});
             else go(std::integral_constant<int, 4>{});
         });
+    };
+    if (m <= kLoraFew) {
+        if (m * lora->rank <= kFuseMost) {
+            ga.first = lora->a;
+            ga.hid_out = hid;
+        } else
+            shrink_small();
         lora_gemm_few(ga, lora->type, y_type, st);
         return check_launch();
     }
@@ -658,16 +672,16 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
     LoraShrinkArgs sa{};
     sa.in = x;
     sa.low = lora->a;
-    sa.order = p.order;
+    sa.rows = p.rows;
     sa.tiles = p.tiles;
     sa.step = x_step;
     sa.out = hid;
-    sa.rows = p.rows;
     sa.hw = ga.hw;
     sa.K = cin;
     sa.rank = lora->rank;
     sa.adapters = lora->adapters;
-    by_adapter_type(lora->type, [&](auto t) {
+    if (m * lora->rank <= kLoraUnsorted) shrink_small();
+    else by_adapter_type(lora->type, [&](auto t) {
         by_rank(lora->rank, false, [&](auto rt, auto it) {
             hipLaunchKernelGGL((lora_shrink_kernel<false, int8_t, decltype(t), decltype(rt)::value, decltype(it)::value>), dim3((unsigned)s.ntiles), dim3(512), 0, st, sa);
         });
@@ -722,14 +736,13 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
     LoraShrinkArgs sa{};
     sa.in = dy;
     sa.low = lora->b;
-    sa.order = p.order;
+    sa.rows = p.rows;
     sa.tiles = p.tiles;
     sa.step = x_step;
     sa.scale = lora->scale;
     sa.w_scale = w_scale;
     sa.out = reinterpret_cast<float *>(ws + s.g);
     sa.out_step = reinterpret_cast<float *>(ws + s.gs);
-    sa.rows = p.rows;
     sa.planes = dx ? reinterpret_cast<bf16_t *>(ws + s.planes) : nullptr;
     sa.hw = hw;
     sa.K = cout;

@@ -86,11 +86,11 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
 }
 
 // ---- the shrinking product: rows of one adapter to `rank` numbers each -------------------------------------
-// A workgroup takes up to 16 I sorted rows of one adapter; its 8 wavefronts share the channels in steps (64 of int8, 32 of
-// real input), every one with all of the rows and ranks, and their sums meet in LDS (8192 x 4096, forward at rank 32 15.6 us, backward with
-// the planes at rank 16 37, 2.2 and 3.6 TB/s).  Bound by the activations' bytes and,
-// from rank 32 on, by the adapter's, which every workgroup reads from L2.  The backward form writes the activations of the next
-// product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as +-2 there), so that dy is read once for both.
+// A workgroup takes up to 16 I sorted rows of one adapter; its 8 wavefronts share the channels in steps of 64, every one with all of the rows
+// and ranks, and their sums meet in LDS.  Bound by the activations' bytes and, from rank 32 on, by the adapter's, which every workgroup reads
+// from L2.  The backward form writes the activations of the next product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as
+// +-2 there), so that dy is read once for both.  8192 x 4096: forward at rank 32 15.6 us (22 where x comes from memory), backward at rank 16 45 us
+// (3.2 TB/s; 50 with steps of 32 channels, whose runs of 64 bytes are half lines).
 struct LoraShrinkArgs {
     const void *in;     // int8 x [m][K] or dy [m][K]
     const void *low;    // [adapters][rank][K]
@@ -119,8 +119,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
 {
     constexpr int PA = planes_of<TA>();
     constexpr int PX = BACK ? planes_of<TX>() : 1;  // (codes: one plane)
-    constexpr int KS = BACK ? 32 : 64;  // channels of a step
-    constexpr int KL = KS / 4;          // of them a lane's
+    constexpr int KS = 64, KL = 16;  // channels of a step, of them a lane's
     __shared__ v4f red[4][I * RT][64];
     const int4 tile = a.tiles[blockIdx.x];
     const int l = tile.x, count = tile.z;
@@ -148,19 +147,19 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * K;
     // U steps of loads leave together before the first of them is used: there are 2 to 4 wavefronts on a SIMD to wait with
     // (rank 32, 8192 x 4096: 20 us with one step at a time)
-    constexpr int U = RT <= 2 ? 4 : RT == 4 ? 2 : 1;
+    constexpr int U = BACK ? (RT == 1 ? (PX == 1 ? 4 : 2) : RT == 2 ? 2 : 1) : RT <= 2 ? 4 : RT == 4 ? 2 : 1;
     auto steps = [&](auto whole, int k, int by, int u) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;
         constexpr int N = WHOLE ? U : 1;
-        Piece<TX, BACK ? 8 : 16> v[N][I];
-        Piece<float, 8> ws[N];
+        Piece<TX, 16> v[N][I];
+        Piece<float, 16> ws[N];
         Piece<TA, 8> w[N][RT][KL / 8];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int k0 = k + (n < u ? n : 0) * by + KL * g;
 #pragma unroll
             for (int i = 0; i < I; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
-            if (BACK && a.planes) ws[n].load_some(a.w_scale + k0, WHOLE ? 8 : K - k0);
+            if (BACK && a.planes) ws[n].load_some(a.w_scale + k0, WHOLE ? 16 : K - k0);
             if (has)
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
@@ -173,20 +172,20 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
         for (int n = 0; n < N; ++n) {
             if (n >= u) break;
             const int k0 = k + n * by + KL * g;
-            v8bf bx[I][BACK ? PX : 2];
+            v8bf bx[I][2][PX];
             if constexpr (BACK) {
                 if (a.planes) {
 #pragma unroll
                     for (int i = 0; i < I; ++i) {
-                        Piece<bf16_t, 8> o[PX];
+                        Piece<bf16_t, 16> o[PX];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
+                        for (int e = 0; e < 16; ++e) {
                             bf16_t s[PX];
                             split<PX>((float)v[n][i].e[e] * ws[n].e[e] * 0.5f, s);
                             // (the decoded codes come in the order 0, 2, 1, 3 of every four)
-                            constexpr int to[8] = {0, 2, 1, 3, 4, 6, 5, 7};
+                            constexpr int to[4] = {0, 2, 1, 3};
 #pragma unroll
-                            for (int p = 0; p < PX; ++p) o[p].e[to[e]] = s[p];
+                            for (int p = 0; p < PX; ++p) o[p].e[(e & ~3) + to[e & 3]] = s[p];
                         }
                         const size_t pos = (size_t)(tile.y + 16 * i + j);
                         if (in[i])
@@ -195,12 +194,19 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < I; ++i) split_piece<PX>(v[n][i], bx[i]);
+                for (int i = 0; i < I; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        Piece<TX, 8> half;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) half.e[e] = v[n][i].e[8 * h + e];
+                        split_piece<PX>(half, bx[i][h]);
+                    }
             } else {
 #pragma unroll
                 for (int i = 0; i < I; ++i) {
-                    bx[i][0] = codes_to_bf16(v[n][i].e);
-                    bx[i][1] = codes_to_bf16(v[n][i].e + 8);
+                    bx[i][0][0] = codes_to_bf16(v[n][i].e);
+                    bx[i][1][0] = codes_to_bf16(v[n][i].e + 8);
                 }
             }
             if (!has) continue;
@@ -212,16 +218,11 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                     split_piece<PA>(w[n][t][h], aw);
 #pragma unroll
                     for (int i = 0; i < I; ++i) {
-                        if constexpr (BACK) {
 #pragma unroll
-                            for (int p = 0; p < PA; ++p)
+                        for (int p = 0; p < PA; ++p)
 #pragma unroll
-                                for (int q = 0; q < PX; ++q)
-                                    if (p + q < 3) acc[i][t] = mfma_bf16(aw[p], bx[i][q], acc[i][t]);
-                        } else {
-#pragma unroll
-                            for (int p = 0; p < PA; ++p) acc[i][t] = mfma_bf16(aw[p], bx[i][h], acc[i][t]);
-                        }
+                            for (int q = 0; q < PX; ++q)
+                                if (p + q < 3) acc[i][t] = mfma_bf16(aw[p], bx[i][h][q], acc[i][t]);
                     }
                 }
         }

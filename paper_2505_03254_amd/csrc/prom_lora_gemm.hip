@@ -13,7 +13,7 @@
 // the 32 deep instruction 16 ranks take the first plane and 16 the second; a second instruction carries the third plane
 // and the factors' second one where the types have them, a third one the product of both second planes.
 // 8192 x 4096 -> 4096: int8 118 us at rank 16 (2.3 Pop/s; the library's plain int8 product reaches 2.2 on this card), bf16 planes 206 to 230
-// (1.2 to 1.33 PF/s; 1.43).  Matrix cores are busy for 50 and 59 % of the time; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
+// (1.2 to 1.33 PF/s; 1.43).  Matrix cores are busy for 50 and 59 % of the clocks; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
 // tiles) and the waits of the two wavefronts of a SIMD for LDS and each other.  Small tiles are chains of latencies: a step takes 0.4 to 0.5 us however little it
 // multiplies.
 #include "prom_lora_gemm.h"

@@ -497,7 +497,7 @@ enum { PROM_F32 = 0, PROM_BF16 = 1, PROM_F16 = 2 };
  * as in prom_pw_conv_dynq), one rounding to y's type at the end.
  * An index outside [0, adapters) means no adapter: the sum over r is left out and hid is zero.  (More than 64 rows are sorted by adapter
  * first, which reads `index` once per adapter; batch elements may come in any order.)  Nothing an adapter
- * holds (infinities, NaN) reaches rows that do not take it.
+ * holds (infinities, NaN) reaches rows that do not take it; in rows that do, an infinite factor may come out as NaN.
  *   a      dev [adapters][rank][cin] of `type` (PROM_BF16 or PROM_F16)
  *   b      dev [adapters][rank][cout] of `type`: row r is the r-th direction in the output channels
  *   scale  dev float32 [adapters];  index dev int32 [n] */

@@ -489,31 +489,33 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
 }
 
 // ---- a few rows -----------------------------------------------------------------------------------------------
-// Up to 64 rows: a workgroup owns 16 channels and all rows, its 8 wavefronts share the input channels 256 at a time, the sums meet in LDS.
+// Up to 64 rows: a workgroup owns 16 CT channels and 16 MT rows, its 8 wavefronts share the input channels 256 at a time, the sums meet in LDS.
 // Four lanes read 64 bytes of a row (and 16 of a channel's codes) in one instruction: every row passes the texture addresser
 // in whole runs.  The low-rank term is one dot product over the ranks per output on the vector ALU, every row with its own adapter; its
 // operands are requested before the product, which they do not depend on.  Bound by latency, then by the adapters' bytes.
 // FUSE: for a token or two every workgroup forms hid itself (rank * cin * 2 bytes a row out of L2, 131 KB at 4096 channels and rank 16, while
 // the product's own loads are on their way) and no launch goes before this one: 9.9 us for 1 token of 4096 -> 4096 against 3.2 + 5.6 in two
 // launches, which cost the host 2 us more.  64 tokens with 64 adapters: 13.7 us.
-template <typename TO, typename TA, int MT, bool FUSE>
+template <typename TO, typename TA, int MT, int CT, bool FUSE>
 __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a)
 {
-    __shared__ v4i red[8][MT][64];
+    __shared__ v4i red[8][CT * MT][64];
     __shared__ float formed[FUSE ? kFuseMost : 1];
     constexpr int RP = 16;  // ranks requested ahead
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int j = lane & 15, g = lane >> 4;
-    const int n0 = logical_block_id() * 16;
+    const int row_blocks = (a.m + 16 * MT - 1) / (16 * MT);  // (workgroups of the same channels are neighbours)
+    const int lid = logical_block_id();
+    const int n0 = lid / row_blocks * 16 * CT, m0 = lid % row_blocks * 16 * MT;
     if (n0 >= a.Nc) return;
     const int K = a.K, KW = a.KW;
 
-    // what the thread will write: row tid / 8, channels n0 + 2 * (tid % 8) and the next
-    const int cc = 2 * (tid & 7), c = n0 + cc;
-    const bool out = tid < 8 * a.m && c < a.Nc;
-    const int row = min(tid >> 3, a.m - 1), channels = out ? a.Nc - c : 0;
+    // what the thread will write: two channels of a row
+    const int mine = tid / (8 * CT), cc = 2 * (tid % (8 * CT)), c = n0 + cc;
+    const bool out = mine < 16 * MT && m0 + mine < a.m && c < a.Nc;
+    const int row = min(m0 + mine, a.m - 1), channels = out ? a.Nc - c : 0;
     const int el = a.hw == 1 ? row : row / a.hw;
     const int l = a.index[el];
     const bool has = out && l >= 0 && l < a.adapters;
@@ -523,25 +525,30 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     Piece<TA, 2> b[RP];
     float h[RP];
     float f = 0.0f;
-    const uint32_t *wrow = a.wq + (size_t)min(n0 + j, a.Nc - 1) * KW;
+    const uint32_t *wrow[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) wrow[t] = a.wq + (size_t)min(n0 + 16 * t + j, a.Nc - 1) * KW;
     const int8_t *xrow[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) xrow[i] = static_cast<const int8_t *>(a.x) + (size_t)min(16 * i + j, a.m - 1) * K;
-    v4i acc[MT];
+    for (int i = 0; i < MT; ++i) xrow[i] = static_cast<const int8_t *>(a.x) + (size_t)min(m0 + 16 * i + j, a.m - 1) * K;
+    v4i acc[CT][MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[t][i] = v4i{0, 0, 0, 0};
     // N steps' loads leave before the first is used; `then` is called between the two
     auto steps = [&](auto whole, auto count, int k, auto then) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;
         constexpr int N = decltype(count)::value;
-        uint32_t w[N][4];
+        uint32_t w[N][CT][4];
         Piece<int8_t, 16> v[N][MT][4];
 #pragma unroll
         for (int s = 0; s < N; ++s)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int k0 = k + 2048 * s + 64 * q + 16 * g;
-                w[s][q] = wrow[WHOLE ? k0 >> 4 : min(k0 >> 4, KW - 1)];  // (past the row's end it meets zeros)
+#pragma unroll
+                for (int t = 0; t < CT; ++t) w[s][t][q] = wrow[t][WHOLE ? k0 >> 4 : min(k0 >> 4, KW - 1)];  // (past the row's end it meets zeros)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) v[s][i][q].load_some(xrow[i] + k0, WHOLE ? 16 : K - k0);
             }
@@ -550,10 +557,13 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
         for (int s = 0; s < N; ++s)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4i A = decode_word_64(w[s][q]);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-                    acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[s][i][q]), acc[i], 0, 0, 0);
+                for (int t = 0; t < CT; ++t) {
+                    const v4i A = decode_word_64(w[s][t][q]);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+                        acc[t][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(A, __builtin_bit_cast(v4i, v[s][i][q]), acc[t][i], 0, 0, 0);
+                }
             }
     };
     using One = std::integral_constant<int, 1>;
@@ -605,7 +615,7 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
                 }
                 if (lane == 0) {
                     formed[p] = s;
-                    if (n0 == 0) a.hid_out[p] = s;
+                    if (lid == 0) a.hid_out[p] = s;
                 }
             }
         }
@@ -624,15 +634,15 @@ __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a
     for (; k < end; k += 2048) steps(std::true_type{}, One{}, k, nothing);
     if (end < K && (end >> 8 & 7) == wave) steps(std::false_type{}, One{}, end, nothing);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
+    for (int i = 0; i < CT * MT; ++i) red[wave][i][lane] = acc[i / MT][i % MT];
     __syncthreads();
     if (!out) return;
     int s0 = 0, s1 = 0;
     {
-        const int from = (row & 15) + 16 * (cc >> 2), e = cc & 3;
+        const int from = (mine & 15) + 16 * (cc >> 2 & 3), e = cc & 3, at = (cc >> 4) * MT + (mine >> 4);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
-            const int *p = reinterpret_cast<const int *>(&red[w][row >> 4][from]) + e;
+            const int *p = reinterpret_cast<const int *>(&red[w][at][from]) + e;
             s0 += p[0];
             s1 += p[1];
         }
@@ -715,11 +725,15 @@ void lora_gemm_few(const LoraGemmArgs &a, int adapter_type, int out_type, hipStr
     by_types(adapter_type, out_type, [&](auto to, auto ta) {
         using TO = decltype(to);
         using TA = decltype(ta);
-        const dim3 grid((unsigned)(((a.Nc + 15) / 16 + 7) / 8 * 8)), block(512);
-        if (a.hid_out) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1, true>), grid, block, 0, st, a);
-        else if (a.m <= 16) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 1, false>), grid, block, 0, st, a);
-        else if (a.m <= 32) hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 2, false>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((lora_gemm_few_kernel<TO, TA, 4, false>), grid, block, 0, st, a);
+        auto go = [&](auto kernel, int rows, int channels) {
+            const int blocks = ((a.Nc + channels - 1) / channels) * ((a.m + rows - 1) / rows);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(512), 0, st, a);
+        };
+        // from 33 rows on 32 x 32 instead of all rows x 16 channels: as many workgroups, and half of the rows' bytes through each
+        if (a.hid_out) go((lora_gemm_few_kernel<TO, TA, 1, 1, true>), 16, 16);  // (32 rows at most, of rank 1: two workgroups per 16 channels)
+        else if (a.m <= 16) go((lora_gemm_few_kernel<TO, TA, 1, 1, false>), 16, 16);
+        else if (a.m <= 32) go((lora_gemm_few_kernel<TO, TA, 2, 1, false>), 32, 16);
+        else go((lora_gemm_few_kernel<TO, TA, 2, 2, false>), 32, 32);
     });
 }
 

@@ -127,6 +127,14 @@ def test_types_and_sizes(P, shape, ti):
     check(P, make(hash(shape) % 1000, *shape, t, dy_type=o), f"{shape} {t} {o} ")
 
 
+@pytest.mark.parametrize("rows,rank", [(1, 32), (2, 16), (3, 10), (16, 2), (17, 1), (31, 1), (32, 1), (33, 1), (5, 7), (33, 20), (48, 128), (64, 5)])
+@pytest.mark.parametrize("cin,cout", [(256, 40), (4640, 33), (70, 16)])
+def test_few_rows(P, rows, rank, cin, cout):
+    """On both sides of what a few rows' product does itself, and of its two shapes."""
+    torch = torch_cuda()
+    check(P, make(rows * rank, rows, 1, 1, cin, cout, rank, 3, torch.bfloat16, dy_type=torch.float32), f"{rows} {rank} ")
+
+
 @pytest.mark.parametrize("rows", [40, 200, 1000])
 @pytest.mark.parametrize("kind", ["none", "one", "last", "outside", "in turn", "runs"])
 def test_who_takes_what(P, rows, kind):

@@ -27,8 +27,8 @@ def test_tiles(P, rows, cin, cout, rank, ti):
 
 
 def test_adapter_layer_beyond_2_31_elements(P):
-    """y and dy of 2.2e9 elements: the first and the last rows against the definition in 64 bits (bf16: 2^-8 relative to the magnitudes
-    of the sums covers both roundings, dy * w_scale and the result)."""
+    """y and dy of 2.2e9 elements: the first and the last rows against the definition in 64 bits, relative to the magnitudes of the sums:
+    y is rounded once (2^-8), with hid in two planes (2^-16) and float32 sums of 68 terms; dx twice (dy * w_scale and the result, 2^-7)."""
     torch = torch_cuda()
     rows, cin, cout, rank = (1 << 20) + 64, 64, 2112, 4
     r = torch.Generator(device="cuda").manual_seed(1)
@@ -53,12 +53,12 @@ def test_adapter_layer_beyond_2_31_elements(P):
         h = (a * real[:, None, :]).sum(2) * has
         want = real @ w.t().contiguous() + (b * h[:, :, None]).sum(1)
         size = real.abs() @ w.abs().t().contiguous() + (b.abs() * h.abs()[:, :, None]).sum(1)
-        assert ((y[at].view(40, cout).to(D) - want).abs() <= 2.0 ** -8 * size).all()
+        assert ((y[at].view(40, cout).to(D) - want).abs() <= (2.0 ** -8 + 2.0 ** -15) * size).all()
         d = dy[at].view(40, cout).to(D)
         g = (b * d[:, None, :]).sum(2) * has
         want = d @ w + (a * g[:, :, None]).sum(1)
         size = d.abs() @ w.abs() + (a.abs() * g.abs()[:, :, None]).sum(1)
-        assert ((dx[at].view(40, cin).to(D) - want).abs() <= 2.0 ** -8 * size).all()
+        assert ((dx[at].view(40, cin).to(D) - want).abs() <= (2.0 ** -7 + 2.0 ** -11) * size).all()
     # db of a million rows in float32: sums of 128 rows, then of their 4000 sums: (128 + 4100) * 2^-24 of the magnitudes
     for l in range(2):
         at = (lora.index == l).nonzero().view(-1)

@@ -65,6 +65,22 @@ template <typename T, int N> struct Piece {
             }
         }
     }
+    // The same by loads without a test each, the first element in the place of absent ones: they are in flight together, where those
+    // of load_some wait for one another (the halves of a register).  It holds N more registers, so only kernels that have them call it.
+    template <typename P> __device__ __forceinline__ void load_some_at_once(P p, int have)
+    {
+        if (have >= N) load(p);
+        else if (have > 0) {
+            T v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = p[i < have ? i : 0];
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = i < have ? v[i] : (T)0.0f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = (T)0.0f;
+        }
+    }
     template <typename P> __device__ __forceinline__ void store_some(P p, int have) const
     {
         if (have >= N) store(p);

@@ -382,7 +382,7 @@ __device__ __forceinline__ void lora_grad_part(const LoraGradBoth &all, const Lo
             const int have = WHOLE ? 8 : chunk.z - m - 8 * g;  // rows of this lane
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[e].load_some(static_cast<const TX *>(a.in) + (size_t)row.e[e] * a.C + c0, WHOLE ? 8 : e < have ? a.C - c0 : 0);
+                v[e].load_some_at_once(static_cast<const TX *>(a.in) + (size_t)row.e[e] * a.C + c0, WHOLE ? 8 : e < have ? a.C - c0 : 0);
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     c[t][e] = 0.0f;

@@ -66,10 +66,12 @@ template <typename T, int N> struct Piece {
         }
     }
     // The same by loads without a test each, the first element in the place of absent ones: they are in flight together, where those
-    // of load_some wait for one another (the halves of a register).  It holds N more registers, so only kernels that have them call it.
+    // of load_some wait for one another (the halves of a register).  It holds N more registers, so only kernels that have them call it:
+    // the adapters' gradients (5341 rows of 513 channels in bf16 24 -> 14 us); the large products spill with it.
     template <typename P> __device__ __forceinline__ void load_some_at_once(P p, int have)
     {
-        if (have >= N) load(p);
+        if constexpr (sizeof(T) == 4) load_some(p, have);  // (a register each: nothing waits there)
+        else if (have >= N) load(p);
         else if (have > 0) {
             T v[N];
 #pragma unroll

@@ -88,9 +88,10 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
 // ---- the shrinking product: rows of one adapter to `rank` numbers each -------------------------------------
 // A workgroup takes up to 16 I sorted rows of one adapter; its 8 wavefronts share the channels in steps of 64, every one with all of the rows
 // and ranks, and their sums meet in LDS.  Bound by the activations' bytes and, from rank 32 on, by the adapter's, which every workgroup reads
-// from L2.  The backward form writes the activations of the next product on the way (dy * w_scale / 2 in bf16 planes; a ternary code reads as
-// +-2 there), so that dy is read once for both.  8192 x 4096: forward at rank 32 15.6 us (22 where x comes from memory), backward at rank 16 45 us
-// (3.2 TB/s; 50 with steps of 32 channels, whose runs of 64 bytes are half lines).
+// from L2.  The backward form writes the activations of the next product on the way (dy * w_scale / 2 in bf16 planes, or for a bf16 dy
+// times the row's factor in f16; a ternary code reads as +-2 there), so that dy is read once for both; the factor needs the row's largest product first,
+// for which the workgroup reads its rows before that.  8192 x 4096: forward at rank 32 15.6 us (22 where x comes from memory), backward at rank 16 in bf16
+// 63 us, 18 of them for the factors.
 struct LoraShrinkArgs {
     const void *in;     // int8 x [m][K] or dy [m][K]
     const void *low;    // [adapters][rank][K]
@@ -101,7 +102,8 @@ struct LoraShrinkArgs {
     const float *w_scale;
     float *out;         // [m][rank]
     float *out_step;    // backward: out * step [m][rank]
-    bf16_t *planes;     // backward: [m positions][P][Kp] or NULL
+    bf16_t *planes;     // backward: [m positions][P][Kp] or NULL (f16 for a bf16 dy)
+    float *down;        // with them for a bf16 dy: [m]
     int hw, K, Kp, rank, adapters;
 };
 
@@ -119,8 +121,12 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
 {
     constexpr int PA = planes_of<TA>();
     constexpr int PX = BACK ? planes_of<TX>() : 1;  // (codes: one plane)
+    constexpr bool SCALED = BACK && kScaledPlane<TX>;
+    using TE = typename std::conditional<SCALED, f16_t, bf16_t>::type;
     constexpr int KS = 64, KL = 16;  // channels of a step, of them a lane's
+    constexpr int BY = KS * 8;       // from one step of a wavefront to its next
     __shared__ v4f red[4][I * RT][64];
+    __shared__ float widest[SCALED ? 8 : 1][16 * I];
     const int4 tile = a.tiles[blockIdx.x];
     const int l = tile.x, count = tile.z;
     if (count == 0) return;
@@ -143,6 +149,53 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[i][t] = v4f{0, 0, 0, 0};
+
+    const int end = K / KS * KS;  // whole steps
+    float up[I];
+    if constexpr (SCALED)
+        if (a.planes) {
+            float most[I];
+#pragma unroll
+            for (int i = 0; i < I; ++i) most[i] = 0.0f;
+            constexpr int M = 4 / I;  // steps whose loads leave together
+            auto look = [&](auto whole, int k, int u) __attribute__((always_inline)) {
+                constexpr bool WHOLE = decltype(whole)::value;
+                constexpr int N = WHOLE ? M : 1;
+                Piece<TX, 16> v[N][I];
+                Piece<float, 16> ws[N];
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const int k0 = k + (n < u ? n : 0) * BY + KL * g;
+#pragma unroll
+                    for (int i = 0; i < I; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
+                    ws[n].load_some(a.w_scale + k0, WHOLE ? 16 : K - k0);
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n)  // (the repeated ones change nothing)
+#pragma unroll
+                    for (int i = 0; i < I; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) most[i] = bits_max(most[i], fabsf((float)v[n][i].e[e] * ws[n].e[e]));
+            };
+            int k = KS * wave;
+            for (; k < end; k += M * BY) look(std::true_type{}, k, min(M, (end - k + BY - 1) / BY));
+            if (end < K && (end / KS & 7) == wave) look(std::false_type{}, end, 1);
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                most[i] = bits_max(most[i], __shfl_xor(most[i], 16, 64));
+                most[i] = bits_max(most[i], __shfl_xor(most[i], 32, 64));
+                if (g == 0) widest[wave][16 * i + j] = most[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float w = widest[0][16 * i + j];
+#pragma unroll
+                for (int o = 1; o < 8; ++o) w = bits_max(w, widest[o][16 * i + j]);
+                up[i] = plane_up(w);
+                if (wave == 0 && g == 0 && in[i]) a.down[row[i]] = plane_down(up[i]);
+            }
+        }
 
     const TA *low = static_cast<const TA *>(a.low) + (size_t)(has ? l : 0) * a.rank * K;
     // U steps of loads leave together before the first of them is used: there are 2 to 4 wavefronts on a SIMD to wait with
@@ -177,11 +230,13 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                 if (a.planes) {
 #pragma unroll
                     for (int i = 0; i < I; ++i) {
-                        Piece<bf16_t, 16> o[PX];
+                        Piece<TE, 16> o[PX];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            bf16_t s[PX];
-                            split<PX>((float)v[n][i].e[e] * ws[n].e[e] * 0.5f, s);
+                            TE s[PX];
+                            const float x = (float)v[n][i].e[e] * ws[n].e[e];
+                            if constexpr (SCALED) s[0] = (f16_t)(x * up[i]);
+                            else split<PX>(x * 0.5f, s);
                             // (the decoded codes come in the order 0, 2, 1, 3 of every four)
                             constexpr int to[4] = {0, 2, 1, 3};
 #pragma unroll
@@ -190,7 +245,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
                         const size_t pos = (size_t)(tile.y + 16 * i + j);
                         if (in[i])
 #pragma unroll
-                            for (int p = 0; p < PX; ++p) o[p].store(a.planes + (pos * PX + p) * a.Kp + k0);
+                            for (int p = 0; p < PX; ++p) o[p].store(reinterpret_cast<TE *>(a.planes) + (pos * PX + p) * a.Kp + k0);
                     }
                 }
 #pragma unroll
@@ -228,8 +283,6 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
         }
     };
     if (BACK || has) {
-        constexpr int BY = KS * 8;  // from one step of a wavefront to its next
-        const int end = K / KS * KS;
         int k = KS * wave;
         for (; k < end; k += U * BY) steps(std::true_type{}, k, BY, min(U, (end - k + BY - 1) / BY));
         // what is left behind the whole steps, and the planes' padding
@@ -522,7 +575,7 @@ template <typename F> static void by_rank(int rank, bool back, F f)
 }
 
 struct LoraSpace {  // offsets into the workspace
-    size_t order, rows, groups, tiles, chunks, hid, g, gs, planes, part_a, part_b, bytes;
+    size_t order, rows, groups, tiles, chunks, hid, g, gs, planes, down, part_a, part_b, bytes;
     int ntiles, nchunks;
 };
 static LoraSpace lora_space(long long m, int n, int cin, int cout, int adapters, int rank, bool back, int planes)
@@ -545,6 +598,7 @@ static LoraSpace lora_space(long long m, int n, int cin, int cout, int adapters,
         s.g = take((size_t)m * rank * 4);
         s.gs = take((size_t)m * rank * 4);
         s.planes = take((size_t)m * planes * lora_padded(cout) * 2);
+        s.down = take(planes == 1 ? (size_t)m * 4 : 0);
         s.part_a = take((size_t)s.nchunks * rank * cin * 4);
         s.part_b = take((size_t)s.nchunks * rank * cout * 4);
     } else
@@ -745,6 +799,7 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
     sa.out = reinterpret_cast<float *>(ws + s.g);
     sa.out_step = reinterpret_cast<float *>(ws + s.gs);
     sa.planes = dx ? reinterpret_cast<bf16_t *>(ws + s.planes) : nullptr;
+    sa.down = reinterpret_cast<float *>(ws + s.down);
     sa.hw = hw;
     sa.K = cout;
     sa.Kp = lora_padded(cout);
@@ -766,6 +821,7 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
         ga.rows = p.rows;
         ga.index = lora->index;
         ga.hid = sa.out;
+        ga.down = sa.down;
         ga.low = lora->a;
         ga.y = dx;
         ga.m = (int)m;

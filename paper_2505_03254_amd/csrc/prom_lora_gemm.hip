@@ -5,15 +5,15 @@
 // 16*PT rows x 64 channels, decodes its own packed codes in registers and reads the rows' operands from two LDS slabs, filled a
 // step ahead.  A step is 128 bytes of every row: 128 int8 or 64 bf16, two matrix instructions deep per accumulator, so
 // that a barrier stands against 2*4*PT of them.
-// A code is two's complement in two bits.  At the top of a byte it reads as 0, 64 or -64; at the top of 16 bits as the bf16 0, 2 or
+// A code is two's complement in two bits.  At the top of a byte it reads as 0, 64 or -64; at the top of 16 bits as the bf16 or f16 0, 2 or
 // -2: decoding is a shift and a mask, 7 instructions for 16 codes in int8 and 15 in bf16.  The sums are 64 (exact in int32)
 // and 2 times too large; the first is shifted back, the second has its half in the input planes.
 // Rows are taken in the order of their adapters, so a wavefront's rows hold few of them: per adapter it loads its channels'
 // factors once and adds hid b with the accumulators as the third operand.  hid goes in as bf16 planes side by side: of
 // the 32 deep instruction 16 ranks take the first plane and 16 the second; a second instruction carries the third plane
 // and the factors' second one where the types have them, a third one the product of both second planes.
-// 8192 x 4096 -> 4096: int8 118 us at rank 16 (2.3 Pop/s; the library's plain int8 product reaches 2.2 on this card), bf16 planes 206 to 230
-// (1.2 to 1.33 PF/s; 1.43).  Matrix cores are busy for 50 and 59 % of the clocks; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
+// 8192 x 4096 -> 4096: int8 118 us at rank 16 (2.3 Pop/s; the library's plain int8 product reaches 2.2 on this card), one plane 212 to 238
+// (1.15 to 1.3 PF/s; 1.43).  Matrix cores are busy for 50 and 59 % of the clocks; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
 // tiles) and the waits of the two wavefronts of a SIMD for LDS and each other.  Small tiles are chains of latencies: a step takes 0.4 to 0.5 us however little it
 // multiplies.
 #include "prom_lora_gemm.h"
@@ -28,7 +28,7 @@ __device__ __forceinline__ v4i decode_word_64(uint32_t w)
 {
     return v4i{(int)((w << 6) & 0xc0c0c0c0u), (int)((w << 4) & 0xc0c0c0c0u), (int)((w << 2) & 0xc0c0c0c0u), (int)(w & 0xc0c0c0c0u)};
 }
-// 8 codes (H: first or second 8 of the 16) as bf16 of twice their values, channels in the order 0, 2, 1, 3 of every four
+// 8 codes (H: first or second 8 of the 16) as bf16 (the same bits as f16) of twice their values, channels in the order 0, 2, 1, 3 of every four
 template <int H> __device__ __forceinline__ v8bf decode_half_bf16(uint32_t w)
 {
     constexpr int d = 2 * H;
@@ -75,7 +75,7 @@ template <int PT, int NW, int KG> struct LoraGeom {
     static constexpr size_t LDS = (size_t)CHANS + TN * 8;
 };
 
-// PLANES: bf16 planes instead of int8 (aligned and padded by their writer).
+// PLANES: planes instead of int8 (aligned and padded by their writer).
 // KG groups of NW wavefronts share the steps of a tile, each with slabs and codes of its own; their sums meet in LDS, and the first group goes on.
 template <int PT, int NW, int KG, bool PLANES, typename TO, typename TA>
 __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGemmArgs a, int ntiles)
@@ -83,6 +83,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
     using G = LoraGeom<PT, NW, KG>;
     constexpr int NQ = G::NQ;
     using Acc = typename std::conditional<PLANES, v4f, v4i>::type;
+    constexpr bool SCALED = PLANES && kScaledPlane<TO>;  // one f16 plane, a factor per row
     extern __shared__ __align__(16) unsigned char all_lds[];
     const int tid = threadIdx.x % G::NT;  // in the group
     const int lane = tid & 63;
@@ -225,6 +226,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
         my_ws = a.w_scale[c];
         if (a.bias) my_bias = a.bias[c];
     }
+    if constexpr (SCALED) my_step = a.down[my_row];
     auto put_info = [&]() __attribute__((always_inline)) {
         if (hhalf == 0 && hrow < G::TM) {
             lrow[hrow] = my_row;
@@ -292,7 +294,10 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
                 if constexpr (PLANES) {
                     const v8bf A = h ? decode_half_bf16<1>(wc[0][t]) : decode_half_bf16<0>(wc[0][t]);
 #pragma unroll
-                    for (int i = 0; i < PT; ++i) acc[i][t] = mfma_bf16(A, __builtin_bit_cast(v8bf, B[i]), acc[i][t]);
+                    for (int i = 0; i < PT; ++i) {
+                        if constexpr (SCALED) acc[i][t] = mfma_f16(__builtin_bit_cast(v8h, A), __builtin_bit_cast(v8h, B[i]), acc[i][t]);
+                        else acc[i][t] = mfma_bf16(A, __builtin_bit_cast(v8bf, B[i]), acc[i][t]);
+                    }
                 } else {
                     const v4i A = decode_word_64(wc[h][t]);
 #pragma unroll
@@ -374,15 +379,16 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
         return __builtin_amdgcn_readfirstlane(next);
     };
     v4f z[PT][4];
+    float st[PT];
+    if constexpr (SCALED || !PLANES)
+#pragma unroll
+        for (int i = 0; i < PT; ++i) st[i] = lstep[16 * i + j];
     if constexpr (PLANES) {
 #pragma unroll
         for (int i = 0; i < PT; ++i)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) z[i][t] = acc[i][t];
+            for (int t = 0; t < 4; ++t) z[i][t] = SCALED ? acc[i][t] * st[i] : acc[i][t];
     } else {
-        float st[PT];
-#pragma unroll
-        for (int i = 0; i < PT; ++i) st[i] = lstep[16 * i + j];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const v4f ws = *reinterpret_cast<const v4f *>(lws + 64 * wave + 16 * t + 4 * g);

@@ -607,12 +607,12 @@ static LoraSpace lora_space(long long m, int n, int cin, int cout, int adapters,
     return s;
 }
 
-static int lora_check(int n, int h, int w, int cin, int cout, const void *wq, const prom_lora_t *lo, long long *m)
+static int lora_check(int n, int h, int w, int cin, int cout, const prom_lora_t *lo, long long *m)
 {
-    if (!lo || !wq || n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0) return PROM_EINVAL;
+    if (!lo || n <= 0 || h <= 0 || w <= 0 || cin <= 0 || cout <= 0) return PROM_EINVAL;
     if (!lo->a || !lo->b || !lo->scale || !lo->index || lo->adapters <= 0 || lo->rank <= 0) return PROM_EINVAL;
     if (lo->type != PROM_BF16 && lo->type != PROM_F16) return PROM_EINVAL;
-    if (misaligned(wq, 4) || misaligned(lo->a, 2) || misaligned(lo->b, 2) || misaligned(lo->scale, 4) || misaligned(lo->index, 4)) return PROM_EINVAL;
+    if (misaligned(lo->a, 2) || misaligned(lo->b, 2) || misaligned(lo->scale, 4) || misaligned(lo->index, 4)) return PROM_EINVAL;
     if (cin > kLoraMaxChannels || cout > kLoraMaxChannels || lo->rank > kLoraMaxRank || lo->adapters > kLoraMaxAdapters) return PROM_EUNSUPPORTED;
     const long long hw = (long long)h * w;
     if (hw > kLoraMaxRows || hw * n > kLoraMaxRows) return PROM_EUNSUPPORTED;
@@ -659,7 +659,8 @@ extern "C" int prom_pw_conv_lora(const int8_t *x, int n, int h, int w, int cin, 
 {
     using namespace prom;
     long long m = 0;
-    if (const int rc = lora_check(n, h, w, cin, cout, w_packed, lora, &m)) return rc;
+    if (!w_packed || misaligned(w_packed, 4)) return PROM_EINVAL;
+    if (const int rc = lora_check(n, h, w, cin, cout, lora, &m)) return rc;
     if (!x || !x_step || !w_scale || !y || (y_type != PROM_F32 && y_type != lora->type)) return PROM_EINVAL;
     const int yb = type_bytes(y_type);
     if (misaligned(x_step, 4) || misaligned(w_scale, 4) || misaligned(bias, 4) || misaligned(y, yb) || misaligned(hid, 4)) return PROM_EINVAL;
@@ -760,7 +761,8 @@ extern "C" int prom_pw_conv_lora_backward(const void *dy, int dy_type, const int
 {
     using namespace prom;
     long long m = 0;
-    if (const int rc = lora_check(n, h, w, cin, cout, dx ? wt_packed : static_cast<const void *>(dy), lora, &m)) return rc;
+    if (dx && (!wt_packed || misaligned(wt_packed, 4))) return PROM_EINVAL;
+    if (const int rc = lora_check(n, h, w, cin, cout, lora, &m)) return rc;
     if (!dy || !x_step || (!dx && !da && !db) || (dx && !w_scale) || (da && !x) || (db && !hid)) return PROM_EINVAL;
     if (dy_type != PROM_F32 && dy_type != lora->type) return PROM_EINVAL;
     const int yb = type_bytes(dy_type), planes = planes_of_type(dy_type);

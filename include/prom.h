@@ -529,7 +529,7 @@ size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, 
  *   dx[m][k]     = sum_co dy[m][co] * w_scale[co] * W[co][k] + sum_r g[m][r] * a[l][r][k]
  *   da[l][r][k]  = sum over the rows m of adapter l of g[m][r] * x_step[i] * x[m][k]
  *   db[l][r][co] = scale[l] * sum over the rows m of adapter l of hid[m][r] * dy[m][co]
- * dx is the gradient of the real activations x * x_step.  Sums in float32 and in a fixed order; dy * w_scale is rounded to 11 bits for a
+ * dx is the gradient of the real activations x * x_step.  Sums in float32, da and db over more than 128 rows in 64 bits, all in a fixed order; dy * w_scale is rounded to 11 bits for a
  * bf16 dy (those below 2^-28 of the row's largest to fewer: the smallest step is 2^-38 of it), 16 for f16, 24 for float32, hid and g to 16 bits
  * for a 16-bit result; all else is exact to float32.
  *   dy, dx     dev [n][h][w][cout] and [n][h][w][cin] of dy_type: PROM_F32 or the adapters' type

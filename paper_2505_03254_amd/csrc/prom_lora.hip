@@ -517,6 +517,8 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(const LoraGradBoth all)
     else lora_grad_part<TX, RT>(all, all.b, blockIdx.y - all.a.blocks);
 }
 
+// An adapter's chunks one after the other, in 64 bits: 2^20 rows are a chain of 8192 additions, which in float32 lose up to 1400 * 2^-24 where the
+// terms are alike.  Bound by the partial sums' bytes either way.
 __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const LoraGradBoth all)
 {
     const int na = all.a.blocks ? (all.a.C + 1023) / 1024 : 0;
@@ -528,17 +530,18 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const LoraGradBoth a
     if (c0 >= C) return;
     const int2 grp = all.groups[l];
     const int base = grp.x / all.chunk + l, chunks = (grp.y + all.chunk - 1) / all.chunk;
-    Piece<float, 4> s;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s.e[e] = 0.0f;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
     for (int k = 0; k < chunks; ++k) {
         Piece<float, 4> v;
         v.load_some(a.part + ((size_t)(base + k) * rank + r) * C + c0, C - c0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s.e[e] += v.e[e];
+        for (int e = 0; e < 4; ++e) s[e] += (double)v.e[e];
     }
-    s.store_some(a.out + ((size_t)l * rank + r) * C + c0, C - c0);
+    Piece<float, 4> o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o.e[e] = (float)s[e];
+    o.store_some(a.out + ((size_t)l * rank + r) * C + c0, C - c0);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------

@@ -670,12 +670,27 @@ def _launch(fn, where, dev, stream, *args):
         raise PromError(rc, where)
 
 
-def _lend(stream, *tensors):
-    """Tensors that a call allocated are used on `stream`: their memory is not handed out again before that work is done."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
+def _on_stream(stream, call, *args):
+    """call(*args) with `stream` current: what it allocates is that stream's memory, whose last user is behind it in the same order, where a block
+    of the current stream's may still be in use there.  Tensors of the caller's that the call works on are not handed out again before `stream` is
+    done with them, nor results before the current stream is."""
+    torch = _torch or _import_torch()
+    dev = args[0].get_device()
+    if dev >= 0 and stream.device.index != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on device {dev}")
+    home = torch.cuda.current_stream(stream.device)
+    if stream == home:
+        return call(*args)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for a in args:
+        for t in (a.a, a.b, a.scale, a.index) if isinstance(a, Lora) else (a,):
+            if isinstance(t, torch.Tensor):
                 t.record_stream(stream)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(home)
+    return out
 
 
 def _out(t, name, like, dtype, shape, dev):
@@ -696,6 +711,8 @@ def _norm_rows(x):
 def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, rstd=None, stream=None):
     """Layer norm over the last dimension of x (float32, bfloat16 or float16; weight and bias float32 or None).
     Returns (y, mean, rstd); mean and rstd float32, one per row."""
+    if stream is not None:
+        return _on_stream(stream, prom_layernorm, x, weight, bias, eps, y, mean, rstd)
     torch = _torch or _import_torch()
     px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
@@ -703,10 +720,9 @@ def prom_layernorm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=No
     y, py = _out(y, "y", x, x.dtype, x.shape, dev)
     mean, pm = _out(mean, "mean", x, f32, by_row, dev)
     rstd, pr = _out(rstd, "rstd", mean, f32, by_row, dev)
-    _launch((_lib or load_library()).prom_layernorm, "prom_layernorm", dev, stream, px, _type_of(x.dtype), rows, cols,
+    _launch((_lib or load_library()).prom_layernorm, "prom_layernorm", dev, None, px, _type_of(x.dtype), rows, cols,
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
             py, pm, pr)
-    _lend(stream, y, mean, rstd)
     return y, mean, rstd
 
 
@@ -714,6 +730,8 @@ def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps
                          stream=None):
     """The same with every row quantised to int8.  Returns (q int8 of x's shape, step, mean, rstd): the real value is
     q * step, row by row."""
+    if stream is not None:
+        return _on_stream(stream, prom_layernorm_quant, x, weight, bias, eps, quant_eps, q, step, mean, rstd)
     torch = _torch or _import_torch()
     px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
@@ -722,10 +740,9 @@ def prom_layernorm_quant(x, weight=None, bias=None, eps: float = 1e-5, quant_eps
     step, ps = _out(step, "step", x, f32, by_row, dev)
     mean, pm = _out(mean, "mean", step, f32, by_row, dev)
     rstd, pr = _out(rstd, "rstd", step, f32, by_row, dev)
-    _launch((_lib or load_library()).prom_layernorm_quant, "prom_layernorm_quant", dev, stream, px, _type_of(x.dtype), rows, cols,
+    _launch((_lib or load_library()).prom_layernorm_quant, "prom_layernorm_quant", dev, None, px, _type_of(x.dtype), rows, cols,
             None if weight is None else _ptr(weight, "weight", f32, by_col, dev), None if bias is None else _ptr(bias, "bias", f32, by_col, dev), eps,
             quant_eps, pq, ps, pm, pr)
-    _lend(stream, q, step, mean, rstd)
     return q, step, mean, rstd
 
 
@@ -741,6 +758,8 @@ def prom_layernorm_backward_workspace_size(dtype, rows: int, cols: int) -> int:
 def prom_layernorm_backward(dy, x, weight, mean, rstd, want_dx: bool = True, want_dweight: bool = True, want_dbias: bool = True,
                             workspace=None, stream=None):
     """Gradients of prom_layernorm.  Returns (dx, dweight, dbias), None for what is not wanted."""
+    if stream is not None:
+        return _on_stream(stream, prom_layernorm_backward, dy, x, weight, mean, rstd, want_dx, want_dweight, want_dbias, workspace)
     torch = _torch or _import_torch()
     px, dev = _input(x, "x")
     rows, cols = _norm_rows(x)
@@ -750,12 +769,11 @@ def prom_layernorm_backward(dy, x, weight, mean, rstd, want_dx: bool = True, wan
     dbias = torch.empty(cols, dtype=f32, device=d) if want_dbias else None
     if workspace is None and (want_dweight or want_dbias):
         workspace = torch.empty(_norm_workspace(t, rows, cols), dtype=torch.uint8, device=d)
-    _launch((_lib or load_library()).prom_layernorm_backward, "prom_layernorm_backward", dev, stream, _ptr(dy, "dy", x.dtype, x.shape, dev), px, t, rows,
+    _launch((_lib or load_library()).prom_layernorm_backward, "prom_layernorm_backward", dev, None, _ptr(dy, "dy", x.dtype, x.shape, dev), px, t, rows,
             cols, None if weight is None else _ptr(weight, "weight", f32, (cols,), dev), _ptr(mean, "mean", f32, by_row, dev),
             _ptr(rstd, "rstd", f32, by_row, dev), dx.data_ptr() if want_dx else None, dweight.data_ptr() if want_dweight else None,
             dbias.data_ptr() if want_dbias else None, None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
             0 if workspace is None else workspace.numel() * workspace.element_size())
-    _lend(stream, dx, dweight, dbias, workspace)
     return dx, dweight, dbias
 
 
@@ -788,6 +806,8 @@ def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora,
                       workspace=None, stream=None):
     """x int8 [n,h,w,cin] device, x_step float32 [n], w_scale float32 [cout], bias float32 [cout] or None.  y is of `dtype`: the adapters' type (default)
     or float32.  Returns y, or (y, hid float32 [n*h*w, rank]) with want_hid or a hid of the caller's."""
+    if stream is not None:
+        return _on_stream(stream, prom_pw_conv_lora, x, w_packed, cout, x_step, w_scale, bias, lora, dtype, y, hid, want_hid, workspace)
     torch = _torch or _import_torch()
     px, dev = _input(x, "x")
     if x.dtype is not torch.int8:
@@ -812,12 +832,11 @@ def prom_pw_conv_lora(x, w_packed, cout: int, x_step, w_scale, bias, lora: Lora,
         workspace = torch.empty(size, dtype=torch.uint8, device=d) if size else None
     if w_packed.numel() * w_packed.element_size() < cout * ((cin + 15) // 16) * 4:
         raise ValueError("w_packed is smaller than the packed form of [cout, cin]")
-    _launch((_lib or load_library()).prom_pw_conv_lora, "prom_pw_conv_lora", dev, stream, px, n, h, w, cin, _ptr(w_packed, "w_packed", None, None, dev),
+    _launch((_lib or load_library()).prom_pw_conv_lora, "prom_pw_conv_lora", dev, None, px, n, h, w, cin, _ptr(w_packed, "w_packed", None, None, dev),
             cout, _ptr(x_step, "x_step", f32, (n,), dev), _ptr(w_scale, "w_scale", f32, (cout,), dev),
             None if bias is None else _ptr(bias, "bias", f32, (cout,), dev), lc, py, _type_of(y.dtype), phid,
             None if workspace is None else _ptr(workspace, "workspace", None, None, dev),
             0 if workspace is None else workspace.numel() * workspace.element_size())
-    _lend(stream, y, hid, workspace)
     return (y, hid) if want_hid else y
 
 
@@ -830,6 +849,8 @@ def prom_pw_conv_lora_backward(dy, x, x_step, wt_packed, w_scale, lora: Lora, hi
                                workspace=None, stream=None):
     """Gradients of prom_pw_conv_lora: dy [n,h,w,cout] float32 or of the adapters' type; wt_packed: prom_pack_ternary of the transposed weights
     [cin, cout].  Returns (dx of dy's type [n,h,w,cin], da, db float32 of the adapters' shapes), None for what is not wanted."""
+    if stream is not None:
+        return _on_stream(stream, prom_pw_conv_lora_backward, dy, x, x_step, wt_packed, w_scale, lora, hid, want_dx, want_da, want_db, workspace)
     torch = _torch or _import_torch()
     px, dev = _input(x, "x")
     if x.dtype is not torch.int8:
@@ -845,13 +866,12 @@ def prom_pw_conv_lora_backward(dy, x, x_step, wt_packed, w_scale, lora: Lora, hi
         workspace = torch.empty(prom_pw_conv_lora_backward_workspace_size(n, h, w, cin, cout, lc.adapters, lc.rank, dy.dtype), dtype=torch.uint8, device=d)
     if want_dx and wt_packed.numel() * wt_packed.element_size() < cin * ((cout + 15) // 16) * 4:
         raise ValueError("wt_packed is smaller than the packed form of [cin, cout]")
-    _launch((_lib or load_library()).prom_pw_conv_lora_backward, "prom_pw_conv_lora_backward", dev, stream, _ptr(dy, "dy", None, (n, h, w, cout), dev),
+    _launch((_lib or load_library()).prom_pw_conv_lora_backward, "prom_pw_conv_lora_backward", dev, None, _ptr(dy, "dy", None, (n, h, w, cout), dev),
             _type_of(dy.dtype), px, n, h, w, cin, None if wt_packed is None else _ptr(wt_packed, "wt_packed", None, None, dev), cout,
             _ptr(x_step, "x_step", f32, (n,), dev), None if w_scale is None else _ptr(w_scale, "w_scale", f32, (cout,), dev), lc,
             None if hid is None else _ptr(hid, "hid", f32, (n * h * w, lc.rank), dev), dx.data_ptr() if want_dx else None,
             da.data_ptr() if want_da else None, db.data_ptr() if want_db else None, _ptr(workspace, "workspace", None, None, dev),
             workspace.numel() * workspace.element_size())
-    _lend(stream, dx, da, db, workspace)
     return dx, da, db
 
 

@@ -909,7 +909,9 @@ class AdamWTensor:
 
 class AdamWTensors:
     """The table of a set of tensors, built and copied to their device once; step() updates all of them with one launch.
-    Keeps references to every tensor it points at."""
+    Keeps references to every tensor it points at; where it runs on a stream for the first time, the table and those tensors are recorded on it, so
+    that their memory is not handed out again before that stream is done with them.  A captured step holds no references: the object has to outlive
+    the graph."""
 
     def __init__(self, tensors):
         torch = _torch or _import_torch()
@@ -928,6 +930,23 @@ class AdamWTensors:
             raise PromError(rc, f"prom_adamw_table (tensor {bad.value})")
         self._table = torch.from_numpy(host).to(self._keep[0].param.device)
         self._table_ptr = self._table.data_ptr()
+        self._streams = {_raw_stream(self._dev)}  # on which the table may be in use
+
+    def _use(self, stream, streams, tensors):
+        """The stream that a launch goes to (None: the current one), if it is none of `streams`: tensors() are recorded on it."""
+        s = _raw_stream(self._dev) if stream is None else int(stream.cuda_stream)
+        if s not in streams:
+            if stream is None:
+                stream = _torch.cuda.current_stream(self._dev)
+            elif stream.device.index != self._dev:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on device {self._dev}")
+            for t in tensors():
+                if t is not None:
+                    t.record_stream(stream)
+            streams.add(s)
+
+    def _all(self):
+        return [self._table] + [v for t in self._keep for v in vars(t).values()]
 
     def step(self, step, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
              grad_scale=None, stream=None):
@@ -946,6 +965,11 @@ class AdamWTensors:
             h.lr = float(lr)
         if grad_scale is not None:
             h.grad_scale = _ptr(grad_scale, "grad_scale", torch.float32, None, dev)
+        if stream is not None:
+            for t in (step, lr, grad_scale):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+        self._use(stream, self._streams, self._all)
         _launch(_lib.prom_adamw_step, "prom_adamw_step", dev, stream, self._table_ptr, self._plan, h)
 
     def moment_targets(self, targets):
@@ -960,12 +984,14 @@ class AdamWTensors:
                 if o.numel() != t.param.numel():
                     raise ValueError("a moment's target must have the parameter's size")
         at = torch.tensor([[m.data_ptr() for m, _ in targets], [v.data_ptr() for _, v in targets]], dtype=torch.int64, device=self._table.device)
-        return targets, at
+        return targets, at, {_raw_stream(self._dev)}
 
     def moments(self, targets, stream=None):
         """The moments of every tensor in float32, into moment_targets(...)."""
-        keep, at = targets
+        keep, at, streams = targets
         p = at.data_ptr()
+        self._use(stream, self._streams, self._all)
+        self._use(stream, streams, lambda: [at] + [t for pair in keep for t in pair])
         _launch(_lib.prom_adamw_moments, "prom_adamw_moments", self._dev, stream, self._table_ptr, self._plan, p, p + 8 * self.count)
         return keep
 

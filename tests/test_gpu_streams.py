@@ -107,3 +107,47 @@ def test_a_captured_pass_with_a_side_stream(P):
         for u, v in zip(got, run()):
             assert torch.equal(u, v)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("how", ["given", "current"])
+def test_a_table_that_nobody_holds_any_more(P, how):
+    """A step and the reading of its moments wait on a busy stream; table and targets' addresses are given back meanwhile."""
+    torch = torch_cuda()
+    sizes = (5000, 33, 257)
+
+    def make():
+        g = torch.Generator().manual_seed(4)
+        return [P.AdamWTensor(torch.randn(n, generator=g).cuda(), torch.randn(n, generator=g).cuda(), torch.zeros(n, dtype=torch.int8, device="cuda"),
+                              torch.zeros(n, dtype=torch.uint8, device="cuda"), *(torch.zeros((n + 255) // 256, device="cuda") for _ in range(2))) for n in sizes]
+
+    def targets():
+        return [(torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")) for n in sizes]
+
+    ref, mref = make(), targets()
+    opt = P.AdamWTensors(ref)
+    opt.step(1)
+    opt.moments(opt.moment_targets(mref))
+    busy, side = Busy(), torch.cuda.Stream()
+    for _ in range(3):
+        got, mgot = make(), targets()
+        opt = P.AdamWTensors(got)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            busy.enqueue()
+        at = opt.moment_targets(mgot)
+        if how == "given":
+            opt.step(1, stream=side)
+            opt.moments(at, stream=side)
+        else:
+            with torch.cuda.stream(side):
+                opt.step(1)
+                opt.moments(at)
+        del opt, at
+        others = [torch.full((k,), 0, dtype=torch.uint8, device="cuda") for k in (24, 48, 128, 256, 512, 1024, 4096) for _ in range(3)]
+        torch.cuda.synchronize()
+        del others
+        for a, b in zip(got, ref):
+            for k in ("param", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale"):
+                assert torch.equal(getattr(a, k), getattr(b, k)), k
+        for a, b in zip(mgot, mref):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

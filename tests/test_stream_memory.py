@@ -140,3 +140,75 @@ def test_a_stream_of_another_device_is_refused(world):
         with pytest.raises(ValueError):
             go(stream=world.side)
     assert not world.launched
+
+
+def tensors(w, n=1000, bits=8):
+    have = lambda k, dtype: Mem(w, (k,), dtype, brought=True)  # noqa: E731
+    m = (torch.int8, torch.uint8) if bits == 8 else (torch.float32, torch.float32)
+    scales = [have((n + 255) // 256, torch.float32) for _ in range(2)] if bits == 8 else []
+    return w.B.AdamWTensor(have(n, torch.float32), have(n, torch.bfloat16), have(n, m[0]), have(n, m[1]), *scales, copy=have(n, torch.bfloat16))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("how", ["given", "current"])
+def test_the_table_of_a_step_on_another_stream(world, how, bits):
+    """The table, which the kernel takes its addresses from, and the tensors that it points at, once for each stream that a step runs on."""
+    w = world
+    home, side, third = w.now[-1], w.side, Stream(0x33)
+    brought = tensors(w, bits=bits)
+    opt = w.B.AdamWTensors([brought])
+    table = next(t for t in w.made if not t.brought)
+
+    def step(s, t):
+        if how == "given":
+            opt.step(t, stream=s)
+        else:
+            w.now.append(s)
+            opt.step(t)
+            w.now.pop()
+
+    opt.step(1)
+    assert not any(t.recorded for t in w.made)
+    step(side, 2)
+    step(side, 3)
+    step(third, 4)
+    opt.step(5)
+    pointed = [t for t in vars(brought).values() if t is not None]
+    for t in [table] + pointed:
+        assert t.recorded == [side, third]
+    assert [h for name, h in w.launched if name == "prom_adamw_step"] == [home.cuda_stream, side.cuda_stream, side.cuda_stream, third.cuda_stream, home.cuda_stream]
+
+
+@pytest.mark.parametrize("how", ["given", "current"])
+def test_the_targets_of_moments_on_another_stream(world, how):
+    w = world
+    home, side = w.now[-1], w.side
+    opt = w.B.AdamWTensors([tensors(w), tensors(w)])
+    pairs = [tuple(Mem(w, (1000,), torch.float32, brought=True) for _ in range(2)) for _ in range(2)]
+    before = len(w.made)
+    targets = opt.moment_targets(pairs)
+    addresses = w.made[before]
+    opt.moments(targets)
+    assert not any(t.recorded for t in w.made)
+    if how == "given":
+        opt.moments(targets, stream=side)
+    else:
+        w.now.append(side)
+        opt.moments(targets)
+        w.now.pop()
+    table = next(t for t in w.made if not t.brought)
+    for t in [table, addresses] + [t for pair in pairs for t in pair]:
+        assert side in t.recorded
+    assert [h for name, h in w.launched if name == "prom_adamw_moments"] == [home.cuda_stream, side.cuda_stream]
+
+
+def test_a_step_on_a_stream_of_another_device_is_refused(world):
+    w = world
+    opt = w.B.AdamWTensors([tensors(w)])
+    targets = opt.moment_targets([tuple(Mem(w, (1000,), torch.float32, brought=True) for _ in range(2))])
+    w.side.device = torch.device("cuda", 1)
+    w.launched.clear()
+    for go in (lambda: opt.step(1, stream=w.side), lambda: opt.moments(targets, stream=w.side)):
+        with pytest.raises(ValueError):
+            go()
+    assert not w.launched

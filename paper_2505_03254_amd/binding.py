@@ -955,16 +955,22 @@ class AdamWTensors:
         torch = _torch
         dev = self._dev
         h = _AdamWHyperC(0.0, beta1, beta2, eps, weight_decay, 0, None, None, None)
+
+        def number(t, name, dtype):
+            if t.numel() == 0:  # (no address: it would stand for a number that the host gives)
+                raise ValueError(f"{name} must hold a number")
+            return _ptr(t, name, dtype, None, dev)
+
         if isinstance(step, torch.Tensor):
-            h.step_dev = _ptr(step, "step", torch.int32, None, dev)
+            h.step_dev = number(step, "step", torch.int32)
         else:
             h.step = int(step)
         if isinstance(lr, torch.Tensor):
-            h.lr_dev = _ptr(lr, "lr", torch.float32, None, dev)
+            h.lr_dev = number(lr, "lr", torch.float32)
         else:
             h.lr = float(lr)
         if grad_scale is not None:
-            h.grad_scale = _ptr(grad_scale, "grad_scale", torch.float32, None, dev)
+            h.grad_scale = number(grad_scale, "grad_scale", torch.float32)
         if stream is not None:
             for t in (step, lr, grad_scale):
                 if isinstance(t, torch.Tensor):

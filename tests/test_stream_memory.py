@@ -212,3 +212,19 @@ def test_a_step_on_a_stream_of_another_device_is_refused(world):
         with pytest.raises(ValueError):
             go()
     assert not w.launched
+
+
+@pytest.mark.parametrize("name,dtype", [("step", torch.int32), ("lr", torch.float32), ("grad_scale", torch.float32)])
+@pytest.mark.parametrize("shape", [(0,), (3, 0)])
+def test_a_hyperparameter_on_the_device_holds_a_number(world, name, dtype, shape):
+    """An empty tensor has no address: as lr it would stand for a rate of 0, as grad_scale for none."""
+    w = world
+    opt = w.B.AdamWTensors([tensors(w)])
+    w.launched.clear()
+    bad = Mem(w, shape, dtype, brought=True)
+    with pytest.raises(ValueError):
+        opt.step(**dict(dict(step=1), **{name: bad}))
+    assert not w.launched
+    for one in ((), (1,), (4,)):
+        opt.step(**dict(dict(step=1), **{name: Mem(w, one, dtype, brought=True)}))
+    assert len(w.launched) == 3

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(const int *__restrict__
 // from L2.  The backward form writes the activations of the next product on the way (dy * w_scale / 2 in bf16 planes, or for a bf16 dy
 // times the row's factor in f16; a ternary code reads as +-2 there), so that dy is read once for both; the factor needs the row's largest product first,
 // for which the workgroup reads its rows before that.  8192 x 4096: forward at rank 32 15.6 us (22 where x comes from memory), backward at rank 16 in bf16
-// 63 us, 18 of them for the factors.
+// 59 us, 14 of them for the factors.
 struct LoraShrinkArgs {
     const void *in;     // int8 x [m][K] or dy [m][K]
     const void *low;    // [adapters][rank][K]
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     constexpr int KS = 64, KL = 16;  // channels of a step, of them a lane's
     constexpr int BY = KS * 8;       // from one step of a wavefront to its next
     __shared__ v4f red[4][I * RT][64];
-    __shared__ float widest[SCALED ? 8 : 1][16 * I];
+    __shared__ float widest[SCALED ? 16 * I : 1];
     const int4 tile = a.tiles[blockIdx.x];
     const int l = tile.x, count = tile.z;
     if (count == 0) return;
@@ -153,46 +153,48 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
     const int end = K / KS * KS;  // whole steps
     float up[I];
     if constexpr (SCALED)
-        if (a.planes) {
-            float most[I];
+        if (a.planes) {  // the rows' largest products, 2 I rows of a wavefront whole and in runs of 1 KB
+            constexpr int R = 2 * I, N = 4 / I;  // N runs' loads leave together
+            if (wave * R < count) {
+                const TX *from[R];
+                float most[R];
 #pragma unroll
-            for (int i = 0; i < I; ++i) most[i] = 0.0f;
-            constexpr int M = 4 / I;  // steps whose loads leave together
-            auto look = [&](auto whole, int k, int u) __attribute__((always_inline)) {
-                constexpr bool WHOLE = decltype(whole)::value;
-                constexpr int N = WHOLE ? M : 1;
-                Piece<TX, 16> v[N][I];
-                Piece<float, 16> ws[N];
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const int k0 = k + (n < u ? n : 0) * BY + KL * g;
-#pragma unroll
-                    for (int i = 0; i < I; ++i) v[n][i].load_some(static_cast<const TX *>(a.in) + (size_t)row[i] * K + k0, WHOLE ? 16 : K - k0);
-                    ws[n].load_some(a.w_scale + k0, WHOLE ? 16 : K - k0);
+                for (int r = 0; r < R; ++r) {
+                    from[r] = static_cast<const TX *>(a.in) + (size_t)a.rows[tile.y + min(wave * R + r, count - 1)] * K;
+                    most[r] = 0.0f;
                 }
+                auto look = [&](auto whole, int k, int u) __attribute__((always_inline)) {
+                    constexpr bool WHOLE = decltype(whole)::value;
+                    constexpr int M = WHOLE ? N : 1;
+                    Piece<TX, 8> v[M][R];
+                    Piece<float, 8> ws[M];
 #pragma unroll
-                for (int n = 0; n < N; ++n)  // (the repeated ones change nothing)
+                    for (int n = 0; n < M; ++n) {
+                        const int k0 = k + 512 * (n < u ? n : 0) + 8 * lane;
 #pragma unroll
-                    for (int i = 0; i < I; ++i)
+                        for (int r = 0; r < R; ++r) v[n][r].load_some_at_once(from[r] + k0, WHOLE ? 8 : K - k0);
+                        ws[n].load_some(a.w_scale + k0, WHOLE ? 8 : K - k0);
+                    }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) most[i] = bits_max(most[i], fabsf((float)v[n][i].e[e] * ws[n].e[e]));
-            };
-            int k = KS * wave;
-            for (; k < end; k += M * BY) look(std::true_type{}, k, min(M, (end - k + BY - 1) / BY));
-            if (end < K && (end / KS & 7) == wave) look(std::false_type{}, end, 1);
+                    for (int n = 0; n < M; ++n)  // (the repeated ones change nothing)
 #pragma unroll
-            for (int i = 0; i < I; ++i) {
-                most[i] = bits_max(most[i], __shfl_xor(most[i], 16, 64));
-                most[i] = bits_max(most[i], __shfl_xor(most[i], 32, 64));
-                if (g == 0) widest[wave][16 * i + j] = most[i];
+                        for (int r = 0; r < R; ++r)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) most[r] = bits_max(most[r], fabsf((float)v[n][r].e[e] * ws[n].e[e]));
+                };
+                const int runs = K & ~511;
+                for (int k = 0; k < runs; k += 512 * N) look(std::true_type{}, k, min(N, (runs - k) >> 9));
+                if (runs < K) look(std::false_type{}, runs, 1);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    most[r] = wave_max_bits(most[r]);
+                    if (lane == 0) widest[wave * R + r] = most[r];
+                }
             }
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                float w = widest[0][16 * i + j];
-#pragma unroll
-                for (int o = 1; o < 8; ++o) w = bits_max(w, widest[o][16 * i + j]);
-                up[i] = plane_up(w);
+                up[i] = plane_up(widest[min(16 * i + j, count - 1)]);
                 if (wave == 0 && g == 0 && in[i]) a.down[row[i]] = plane_down(up[i]);
             }
         }
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(const LoraShrinkArgs a
 
 // The same for fewer rows, without sorting: a wavefront per row and RC ranks, the channels over its lanes, float32 on the vector
 // ALU.  Every row reads its own adapter; what bounds it is the latency of two dependent loads and, with many rows, the adapters' bytes (64 rows of
-// 4096 channels, rank 16, 64 adapters: 4.0 us).
+// 4096 channels, rank 16, 64 adapters: 5.9 us).
 template <typename TA, int RC>
 __global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__restrict__ x, const TA *__restrict__ low, const int *__restrict__ index,
                                                                 const float *__restrict__ step, float *__restrict__ hid, int m, int hw, int K,
@@ -386,7 +388,7 @@ __global__ __launch_bounds__(256) void lora_shrink_small_kernel(const int8_t *__
 // its own registers (pairs of rows by v_perm); it then holds 8 rows of its 8 columns, which is one operand for each of
 // 8 tiles whose 16 columns lie 8 apart: no LDS, whole runs of 8 bytes (int8) or 16 to 32 a lane.  A workgroup takes 512 columns and a chunk
 // of one adapter's sorted rows, and writes partial sums; a second kernel adds an adapter's chunks in their order.  8192 rows of 4096 int8
-// and 4096 bf16 columns, rank 16: 35 us and 9 for the sums; bound by the latency of gathered rows, two steps ahead at most.
+// and 4096 bf16 columns, rank 16: 38 us and 10 for the sums; bound by the latency of gathered rows, two steps ahead at most.
 struct LoraGradArgs {
     const void *in;      // [m][C]
     const float *coef;   // [m][rank]
@@ -548,8 +550,8 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const LoraGradBoth a
 static size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 // Rows of a chunk of the adapters' gradients.  More chunks keep more loads on their way, and every one costs rank * (cin + cout) * 4 bytes of
-// partial sums, written and read: 8192 x 4096 -> 4096, rank 16, both gradients with their sums 44 us with 128 rows, 51 with 256, 54 with 512;
-// 500 x 1000 -> 1030 in float32 22, 26 and 25.
+// partial sums, written and read: 8192 x 4096 -> 4096, rank 16, both gradients with their sums 47 us with 128 rows, 47 with 256, 64 with 512;
+// 500 x 1000 -> 1030 in float32 22, 29 and 29.
 constexpr int kLoraChunk = 128;
 
 template <typename F> static void by_adapter_type(int type, F f)
@@ -564,7 +566,8 @@ template <typename F> static void by_real_type(int type, F f)
 }
 // Rows of a workgroup of the shrinking product.  Forward 32: every workgroup reads the adapter again, from rank 16 on as many bytes as
 // its activations are (8192 x 4096, rank 32: 15.6 us, with 16 rows 22.7).  Backward 16 up to rank 32, where the
-// activations are twice the bytes, written once more: more workgroups keep more of them on their way (rank 16: 36.7 us, with 32 rows 43.2).
+// activations are twice the bytes, written once more: more workgroups keep more of them on their way (8192 x 4096 in bf16 at
+// rank 16: 59 us, with 32 rows 66; 500 x 1030 in float32 at rank 12 11.6 and 17.4).
 static int lora_tile(int rank, bool back) { return back && rank <= 32 ? 16 : 32; }
 // f(rank tiles of 16, row tiles of 16)
 template <typename F> static void by_rank(int rank, bool back, F f)

@@ -494,7 +494,7 @@ enum { PROM_F32 = 0, PROM_BF16 = 1, PROM_F16 = 2 };
  *   hid[m][r] = x_step[i] * sum_k x[m][k] * a[l][r][k]
  *   y[m][co]  = (acc[m][co] * w_scale[co]) * x_step[i] + bias[co] + scale[l] * sum_r hid[m][r] * b[l][r][co]
  * acc the int32 accumulator of prom_pw_conv, everything real in float32 (up to the bias three operations, each rounded once,
- * as in prom_pw_conv_dynq), one rounding to y's type at the end.
+ * as in prom_pw_conv_dynq), one rounding to y's type at the end; above 64 rows scale * hid enters a 16-bit y with 16 bits.
  * An index outside [0, adapters) means no adapter: the sum over r is left out and hid is zero.  (More than 64 rows are sorted by adapter
  * first, which reads `index` once per adapter; batch elements may come in any order.)  Nothing an adapter
  * holds (infinities, NaN) reaches rows that do not take it; in rows that do, an infinite factor may come out as NaN.
@@ -529,9 +529,9 @@ size_t prom_pw_conv_lora_workspace_size(int n, int h, int w, int cin, int cout, 
  *   dx[m][k]     = sum_co dy[m][co] * w_scale[co] * W[co][k] + sum_r g[m][r] * a[l][r][k]
  *   da[l][r][k]  = sum over the rows m of adapter l of g[m][r] * x_step[i] * x[m][k]
  *   db[l][r][co] = scale[l] * sum over the rows m of adapter l of hid[m][r] * dy[m][co]
- * dx is the gradient of the real activations x * x_step.  Sums in float32, da and db over more than 128 rows in 64 bits, all in a fixed order; dy * w_scale is rounded to 11 bits for a
- * bf16 dy (those below 2^-28 of the row's largest to fewer: the smallest step is 2^-38 of it), 16 for f16, 24 for float32, hid and g to 16 bits
- * for a 16-bit result; all else is exact to float32.
+ * dx is the gradient of the real activations x * x_step.  Sums in float32, da and db over more than 128 rows in 64 bits, all in a fixed order.
+ * In dx dy * w_scale is rounded to 11 bits for a bf16 dy (those below 2^-28 of the row's largest to fewer: the smallest step is 2^-38 of it), 16
+ * for f16, 24 for float32, and g to 16 bits where dx has 16; all else is exact to float32.
  *   dy, dx     dev [n][h][w][cout] and [n][h][w][cin] of dy_type: PROM_F32 or the adapters' type
  *   wt_packed  dev, prom_pack_ternary output of the TRANSPOSED weights [cin][cout] (once per layer; not looked at without dx)
  *   hid        dev float32 [n*h*w][rank], from the forward call (not looked at without db); x is not looked at without da
@@ -560,7 +560,7 @@ int prom_layernorm(const void *x, int type, long long rows, int cols, const floa
  * (mean and rstd summed in float64 and rounded once, so that no code depends on the order of a sum)
  *   top = max(max_c |y|, quant_eps),  q = clamp(round_half_even(y * (127 / top)), -128, 127),  step = top / 127
  *   q  dev int8 [rows][cols];  step dev float32 [rows]: the real value is q * step.
- * A row with a NaN gets the step NaN, one with an infinity an infinite or NaN step; their codes mean nothing. */
+ * quant_eps > 0; 127 / top has to be finite (top 2^-121 and more).  A row with a NaN gets the step NaN, one with an infinity an infinite or NaN step; their codes mean nothing. */
 int prom_layernorm_quant(const void *x, int type, long long rows, int cols, const float *weight, const float *bias, float eps,
                          float quant_eps, int8_t *q, float *step, float *mean, float *rstd, void *stream);
 

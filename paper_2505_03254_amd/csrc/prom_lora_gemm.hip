@@ -1,4 +1,4 @@
-// y = (rows x ternary weights) scaled, plus the rows' low-rank terms: the product behind prom_pw_conv_lora and, on bf16 planes,
+// y = (rows x ternary weights) scaled, plus the rows' low-rank terms: the product behind prom_pw_conv_lora and, on 16-bit planes,
 // the gradient of its activations.
 //
 // Tiled kernel.  As in the kernel of wide layers (prom_pw_gemm.hip) the k loop is outermost over a workgroup's tile, a wavefront owns
@@ -12,8 +12,8 @@
 // factors once and adds hid b with the accumulators as the third operand.  hid goes in as bf16 planes side by side: of
 // the 32 deep instruction 16 ranks take the first plane and 16 the second; a second instruction carries the third plane
 // and the factors' second one where the types have them, a third one the product of both second planes.
-// 8192 x 4096 -> 4096: int8 118 us at rank 16 (2.3 Pop/s; the library's plain int8 product reaches 2.2 on this card), one plane 212 to 238
-// (1.15 to 1.3 PF/s; 1.43).  Matrix cores are busy for 50 and 59 % of the clocks; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
+// 8192 x 4096 -> 4096: int8 118 us at rank 16 (2.3 Pop/s; the library's plain int8 product reaches 2.2 on this card), one plane 207 to 241
+// (1.14 to 1.33 PF/s; 1.43).  Matrix cores are busy for 39 % (rank 32) and 48 % of the nominal clock's cycles; the rest is the ends of a tile (every 16 ranks 3 to 4 us a round of
 // tiles) and the waits of the two wavefronts of a SIMD for LDS and each other.  Small tiles are chains of latencies: a step takes 0.4 to 0.5 us however little it
 // multiplies.
 #include "prom_lora_gemm.h"
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(64 * NW * KG, 2) void lora_gemm_kernel(const LoraGe
 // in whole runs.  The low-rank term is one dot product over the ranks per output on the vector ALU, every row with its own adapter; its
 // operands are requested before the product, which they do not depend on.  Bound by latency, then by the adapters' bytes.
 // FUSE: for a token or two every workgroup forms hid itself (rank * cin * 2 bytes a row out of L2, 131 KB at 4096 channels and rank 16, while
-// the product's own loads are on their way) and no launch goes before this one: 9.9 us for 1 token of 4096 -> 4096 against 3.2 + 5.6 in two
+// the product's own loads are on their way) and no launch goes before this one: 10.2 us for 1 token of 4096 -> 4096 against 3.2 + 5.6 in two
 // launches, which cost the host 2 us more.  64 tokens with 64 adapters: 12.3 us.
 template <typename TO, typename TA, int MT, int CT, bool FUSE>
 __global__ __launch_bounds__(512) void lora_gemm_few_kernel(const LoraGemmArgs a)

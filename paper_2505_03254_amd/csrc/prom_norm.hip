@@ -8,7 +8,8 @@
 // All three are bound by the bytes of their rows.  A row is read once and stays in registers: WPR wavefronts own it, NV
 // pieces of 16 bytes per lane, so that every load of a row is in flight at once and the moments, which need the
 // whole row before the first output, cost no second read.  The sum of squares is taken around the mean (the row is
-// there), never as a difference of large sums.  Measured: 1 x 4096 in f16 3.0 us (latency), 2048 x 2048 bf16 into int8 7.7 us.
+// there), never as a difference of large sums.  Measured: 1 x 4096 in f16 3.2 us (latency), 2048 x 2048 bf16 into int8 8.9 us
+// (1.5 TB/s: two wavefronts on a SIMD, and three reductions in a row, two of them in 64 bits).
 #include "prom.h"
 #include "prom_float.h"
 #include "prom_launch.h"
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void norm_kernel(const NormArgs 
 // to row (each lane owns its columns in all of them); they meet in LDS once at the end and leave as one row of
 // partial sums per workgroup.  A second kernel adds the rows up in their order: no atomics, the same bits every time.
 // The next row is on its way while one is worked on (up to two pieces a lane; more of them fill the registers).
-// 8192 x 4096 bf16: 38.4 us and 5.2 for the sums where the rows still lie in the last-level cache, 47.7 from memory, 4.4 TB/s (with 4
+// 8192 x 4096 bf16: 38.4 us and 5.2 for the sums where the rows still lie in the last-level cache, 48.4 and 5.4 from memory, 4.4 TB/s (with 4
 // wavefronts of whole rows, 8 pieces a lane and no row ahead 117 us).
 struct NormGradArgs {
     const void *dy, *x;

@@ -941,7 +941,7 @@ class AdamWTensors:
             elif stream.device.index != self._dev:
                 raise ValueError(f"the stream is on {stream.device}, the tensors on device {self._dev}")
             for t in tensors():
-                if t is not None:
+                if isinstance(t, _torch.Tensor):
                     t.record_stream(stream)
             streams.add(s)
 

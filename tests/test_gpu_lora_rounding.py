@@ -61,6 +61,24 @@ def test_a_large_element_beside_small_ones(P):
     assert ((dx - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 308 * 2.0 ** -24) * size).all()
 
 
+@pytest.mark.parametrize("e", [24, 28, 32, 36])
+def test_elements_far_below_the_rows_largest(P, e):
+    """2^-28 of the largest product and less is held in steps of 2^-38 of it, half of one off at most per term, and not as zero."""
+    torch = torch_cuda()
+    r = torch.Generator().manual_seed(e)
+    dy = (1 + torch.rand(70, 200, generator=r)).bfloat16()
+    dy[:, 3] = 2.0 ** e
+    codes = torch.randint(0, 2, (200, 40), generator=r, dtype=torch.int8)
+    codes[3] = 0
+    codes[3, 20:] = 1
+    dx = dx_alone(P, dy, codes, torch.ones(200)).double()
+    want = dy.double() @ codes.double()
+    terms = codes.double().sum(0)
+    lost = 2.0 ** (e - 39) * terms if e >= 28 else 0.0 * terms
+    assert ((dx - want).abs() <= (2.0 ** -8 + 208 * 2.0 ** -24) * want + 2.0 ** -11 * want + lost).all()
+    assert (dx[:, :20] > 0.5 * want[:, :20]).all()
+
+
 def test_rows_of_zeros_and_rows_that_are_not_finite(P):
     torch = torch_cuda()
     r = torch.Generator().manual_seed(2)
